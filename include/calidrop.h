@@ -436,6 +436,112 @@ int calidrop_recalibrate_packed(const calidrop_params* p, const void* q_t, const
                                 const float* a_lse, void* out, float* c_q, float* c_out,
                                 float* c_lse, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * A cache in pages, ahead of or next to compression.
+ *
+ * k_pages, v_pages hold n_pages pages of page_size rows of every KV head, [n_pages][Hkv][page_size][D]: a page is laid out
+ * like a prompt or a compressed cache of page_size rows.  (Prompts of one length n kept in pages of n rows, in order, are
+ * the packed prompts calidrop_compress reads; compressed caches of one capacity are pages of that many rows.)
+ * page_table [batch][max_pages] int32 (device) names the pages of each sequence: row r is row r % page_size of page
+ * page_table[b][r / page_size].  Entries behind the last row a call needs are not read, nor are those of rows that no query
+ * of a call sees under a window.  The tables are device memory, so the host cannot check them: rows on an entry outside
+ * [0, n_pages) are not written by calidrop_paged_append and read as some existing page by the attention calls - memory safe,
+ * result meaningless.  K and V rows that a query of a call sees must be finite; what other rows hold does not matter.
+ *
+ * Tokens of a call are packed: those of sequence b are offsets[b] .. offsets[b+1]-1 (any number, none included), where NULL
+ * offsets mean one token per sequence (then the total must be batch).  Tokens that no sequence owns (behind the last one)
+ * are neither read nor written.
+ */
+typedef enum {
+  CALIDROP_ROT_HALVES = 0,     /* element j of the rotated part is paired with element j + rot_dim / 2 */
+  CALIDROP_ROT_NEIGHBOURS = 1  /* element 2 j with element 2 j + 1                                     */
+} calidrop_rot_pairs;
+
+typedef struct {
+  uint32_t struct_size; /* = sizeof(calidrop_paged_params)                                    */
+  int32_t dtype;        /* calidrop_dtype of queries, pages and outputs                       */
+  int32_t batch;        /* sequences, at most 65535                                           */
+  int32_t n_q_heads, n_kv_heads, head_dim; /* as in calidrop_params                           */
+  int32_t page_size;    /* rows of a page, any number >= 1                                    */
+  int32_t n_pages;      /* pages in k_pages and in v_pages; n_pages * Hkv * page_size < 2^32  */
+  int32_t max_pages;    /* entries of a sequence in page_table                                */
+  float scale;          /* logit scale; 0 selects 1/sqrt(D)                                   */
+  int32_t window;       /* attention: 0 = a query sees every row up to its own; W >= 1 = its own and
+                           the W - 1 rows before it                                           */
+  int32_t sinks;        /* with a window, the first `sinks` rows stay visible too             */
+  int32_t rot_dim;      /* append: leading elements of a head that are rotated, a multiple of 16,
+                           at most D; 0 = none                                                */
+  int32_t rot_pairs;    /* calidrop_rot_pairs                                                 */
+} calidrop_paged_params;
+
+/*
+ * calidrop_paged_append - new keys and values to the ends of the caches, rotated by their positions on the way; the
+ * queries of the same tokens rotated alongside.
+ *
+ * Token t of sequence b becomes row cache_lens[b] + t of its cache.  A pair (x, y) of the first rot_dim elements of its
+ * query and key heads becomes (x cos - y sin, y cos + x sin) with the angle of its position, in fp32, rounded once to
+ * dtype; other elements, and v, are copied.  new_lens[b] = cache_lens[b] + its tokens.  A sequence whose new rows do not
+ * fit its max_pages * page_size rows is left unchanged (no row written, new_lens[b] = cache_lens[b]); its queries are
+ * rotated all the same.
+ *
+ * Arguments
+ *   q, k, v       [total_new][Hq or Hkv][D] dtype, consecutive tokens q_stride / k_stride / v_stride elements apart (parts of
+ *                 one projection's output, say): a multiple of 16 bytes, at least heads * D.  q may be NULL (with q_out).
+ *   new_offsets   [batch+1] int32 or NULL; max_new >= the tokens of every sequence (host copy; sizes the grid).
+ *   positions     [total_new] int32, or NULL: the row in the cache.
+ *   rot_table     fp32 [n_positions][rot_dim]: the cosines of position p's rot_dim / 2 angles, then their sines.  Positions
+ *                 outside [0, n_positions) take the nearest entry.  NULL when rot_dim = 0.
+ *   q_out         out [total_new][Hq][D] dtype; may be q itself when q_stride = Hq * D.
+ *   new_lens      out [batch] int32; may be cache_lens itself.
+ * No workspace.
+ */
+int calidrop_paged_append(const calidrop_paged_params* p, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                          const void* v, int64_t v_stride, const int32_t* new_offsets, int64_t total_new, int32_t max_new,
+                          const int32_t* positions, const float* rot_table, int32_t n_positions, void* k_pages,
+                          void* v_pages, const int32_t* page_table, const int32_t* cache_lens, int32_t* new_lens,
+                          void* q_out, void* stream);
+
+/*
+ * calidrop_paged_attend - attention of the newest tokens of every sequence over its cache: a whole prompt, the next chunk of
+ * one, or single tokens.
+ *
+ * The nq tokens of sequence b in the call are the last nq of its L = cache_lens[b] rows: token t stands at row
+ * i = L - nq + t and sees the rows j <= i with window = 0, j > i - window, or j < sinks.  Per query head h (KV head
+ * g = h / G): lse = log sum_j exp(scale q.K_j), out = sum_j exp(scale q.K_j - lse) V_j.  A token that sees no row (i < 0)
+ * gets out = 0, lse = -inf.
+ *
+ *   q             [total_q][Hq][D] dtype.    q_offsets  [batch+1] int32 or NULL.
+ *   cache_lens    [batch] int32, rows of each cache including the tokens of this call; max_q_len >= the tokens and
+ *                 max_cache_len >= the rows of every sequence (host copies; a longer cache is cut off there).
+ *   out           out [total_q][Hq][D] dtype.    lse  out [total_q][Hq] fp32, natural log (the rows of the last tokens are
+ *                 the win_lse of calidrop_compress_with_lse).
+ *   workspace     >= calidrop_paged_attend_workspace_bytes(p, total_q, max_q_len, max_cache_len) bytes, 256-byte aligned;
+ *                 the size does not fall as any of the three grows.
+ */
+size_t calidrop_paged_attend_workspace_bytes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len,
+                                             int32_t max_cache_len);
+int calidrop_paged_attend(const calidrop_paged_params* p, const void* q, const int32_t* q_offsets, int64_t total_q,
+                          int32_t max_q_len, const void* k_pages, const void* v_pages, const int32_t* page_table,
+                          const int32_t* cache_lens, int32_t max_cache_len, void* out, float* lse, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * calidrop_paged_attend_shared - the same for sequences that continue one prefix: every token sees the shared_len rows of the
+ * prefix, then the rows of its own cache as in calidrop_paged_attend (cache_lens counts those alone).  The prefix is read
+ * once for all queries instead of once per sequence.
+ *
+ *   shared_table  [ceil(shared_len / page_size)] int32 (device): the pages of the prefix, in k_pages and v_pages.
+ *   shared_len    >= 1.  window and sinks must be 0 (CALIDROP_EUNSUPPORTED).
+ * Everything else as in calidrop_paged_attend; the workspace size does not fall as any of the four numbers grows.
+ */
+size_t calidrop_paged_attend_shared_workspace_bytes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len,
+                                                    int32_t max_cache_len, int32_t shared_len);
+int calidrop_paged_attend_shared(const calidrop_paged_params* p, const void* q, const int32_t* q_offsets, int64_t total_q,
+                                 int32_t max_q_len, const void* k_pages, const void* v_pages, const int32_t* shared_table,
+                                 int32_t shared_len, const int32_t* page_table, const int32_t* cache_lens,
+                                 int32_t max_cache_len, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
 /* Host string describing the last error on the calling thread ("" if none). Never NULL.      */
 const char* calidrop_last_error(void);
 

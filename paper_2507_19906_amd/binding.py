@@ -18,6 +18,7 @@ BF16, FP32 = 0, 1
 FLAG_NONE, FLAG_CALIBRATED, FLAG_RECOMPUTE, FLAG_RECOMPUTED = 0, 1, 2, 3
 REGION_ROW_LSE, REGION_SCORE, REGION_VOTE_PLANES, REGION_ROW_PARTS = 0, 1, 2, 3
 OPT_WRITE_SCORES, OPT_WIDE_SELECTION = 1, 2
+ROT_HALVES, ROT_NEIGHBOURS = 0, 1
 
 
 class CalidropError(RuntimeError):
@@ -46,6 +47,26 @@ class Params(ctypes.Structure):
     ]
 
 
+class PagedParams(ctypes.Structure):
+    """Mirror of calidrop_paged_params."""
+    _fields_ = [
+        ("struct_size", ctypes.c_uint32),
+        ("dtype", ctypes.c_int32),
+        ("batch", ctypes.c_int32),
+        ("n_q_heads", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("window", ctypes.c_int32),
+        ("sinks", ctypes.c_int32),
+        ("rot_dim", ctypes.c_int32),
+        ("rot_pairs", ctypes.c_int32),
+    ]
+
+
 def make_params(*, dtype, batch, n_q_heads, n_kv_heads, head_dim, window, budget, pool_kernel,
                 scale=0.0, theta1=0.7, theta2=0.85, calib_size=0, flags=0) -> Params:
     if isinstance(dtype, torch.dtype):
@@ -54,6 +75,18 @@ def make_params(*, dtype, batch, n_q_heads, n_kv_heads, head_dim, window, budget
         dtype = BF16 if dtype == "bf16" else FP32
     return Params(ctypes.sizeof(Params), dtype, batch, n_q_heads, n_kv_heads, head_dim, window,
                   budget, pool_kernel, scale, theta1, theta2, calib_size, flags)
+
+
+def make_paged_params(*, dtype, batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages, scale=0.0, window=0,
+                      sinks=0, rot_dim=0, rot_pairs=ROT_HALVES) -> PagedParams:
+    if isinstance(dtype, torch.dtype):
+        dtype = {torch.bfloat16: BF16, torch.float32: FP32}.get(dtype, -1)
+    elif isinstance(dtype, str):
+        dtype = {"bf16": BF16, "fp32": FP32}.get(dtype, -1)
+    if isinstance(rot_pairs, str):
+        rot_pairs = {"halves": ROT_HALVES, "neighbours": ROT_NEIGHBOURS}.get(rot_pairs, -1)
+    return PagedParams(ctypes.sizeof(PagedParams), dtype, batch, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, max_pages,
+                       scale, window, sinks, rot_dim, rot_pairs)
 
 
 _lib = None
@@ -121,6 +154,18 @@ def lib() -> ctypes.CDLL:
         L.calidrop_compress_h2o.restype = ctypes.c_int
         L.calidrop_compress_h2o.argtypes = [pp, i32, vp, vp, vp, vp, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                             vp, sz, vp]
+        qq = ctypes.POINTER(PagedParams)
+        L.calidrop_paged_append.restype = ctypes.c_int
+        L.calidrop_paged_append.argtypes = [qq, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, vp, i32, vp, vp,
+                                            vp, vp, vp, vp, vp]
+        L.calidrop_paged_attend_workspace_bytes.restype = sz
+        L.calidrop_paged_attend_workspace_bytes.argtypes = [qq, i64, i32, i32]
+        L.calidrop_paged_attend.restype = ctypes.c_int
+        L.calidrop_paged_attend.argtypes = [qq, vp, vp, i64, i32, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+        L.calidrop_paged_attend_shared_workspace_bytes.restype = sz
+        L.calidrop_paged_attend_shared_workspace_bytes.argtypes = [qq, i64, i32, i32, i32]
+        L.calidrop_paged_attend_shared.restype = ctypes.c_int
+        L.calidrop_paged_attend_shared.argtypes = [qq, vp, vp, i64, i32, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp, sz, vp]
         L.calidrop_append.restype = ctypes.c_int
         L.calidrop_append.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp]
         _lib = L
@@ -457,6 +502,154 @@ class EvictedStore:
             return self.evict_indices[lo:lo + cap * Hkv].view(Hkv, cap)
         t = self.k_e if which == "k" else self.v_e
         return t[lo * D:(lo + cap * Hkv) * D].view(Hkv, cap, D)
+
+
+def calidrop_paged_append(p: PagedParams, q, q_stride: int, k, k_stride: int, v, v_stride: int, new_offsets, total_new: int,
+                          max_new: int, positions, rot_table, n_positions: int, k_pages, v_pages, page_table, cache_lens,
+                          new_lens, q_out, stream=None) -> None:
+    _check(lib().calidrop_paged_append(
+        ctypes.byref(p), _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(new_offsets), total_new, max_new,
+        _ptr(positions), _ptr(rot_table), n_positions, _ptr(k_pages), _ptr(v_pages), _ptr(page_table), _ptr(cache_lens),
+        _ptr(new_lens), _ptr(q_out), _stream(stream)))
+
+
+def calidrop_paged_attend_workspace_bytes(p: PagedParams, total_q: int, max_q_len: int, max_cache_len: int) -> int:
+    n = lib().calidrop_paged_attend_workspace_bytes(ctypes.byref(p), total_q, max_q_len, max_cache_len)
+    if n == 0:
+        raise CalidropError(EINVAL, calidrop_last_error())
+    return n
+
+
+def calidrop_paged_attend(p: PagedParams, q, q_offsets, total_q: int, max_q_len: int, k_pages, v_pages, page_table, cache_lens,
+                          max_cache_len: int, out, lse, workspace, stream=None) -> None:
+    _check(lib().calidrop_paged_attend(
+        ctypes.byref(p), _ptr(q), _ptr(q_offsets), total_q, max_q_len, _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
+        _ptr(cache_lens), max_cache_len, _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+
+
+def calidrop_paged_attend_shared_workspace_bytes(p: PagedParams, total_q: int, max_q_len: int, max_cache_len: int,
+                                                 shared_len: int) -> int:
+    n = lib().calidrop_paged_attend_shared_workspace_bytes(ctypes.byref(p), total_q, max_q_len, max_cache_len, shared_len)
+    if n == 0:
+        raise CalidropError(EINVAL, calidrop_last_error())
+    return n
+
+
+def calidrop_paged_attend_shared(p: PagedParams, q, q_offsets, total_q: int, max_q_len: int, k_pages, v_pages, shared_table,
+                                 shared_len: int, page_table, cache_lens, max_cache_len: int, out, lse, workspace,
+                                 stream=None) -> None:
+    _check(lib().calidrop_paged_attend_shared(
+        ctypes.byref(p), _ptr(q), _ptr(q_offsets), total_q, max_q_len, _ptr(k_pages), _ptr(v_pages), _ptr(shared_table),
+        shared_len, _ptr(page_table), _ptr(cache_lens), max_cache_len, _ptr(out), _ptr(lse), _ptr(workspace), _nbytes(workspace),
+        _stream(stream)))
+
+
+class PagedCache:
+    """A cache in pages: the tensors of one and the calls on it.  It checks what the library cannot see behind a pointer
+    (shapes, types, layouts, the device) and refuses what does not fit with ValueError.
+
+    k_pages, v_pages [n_pages][Hkv][page_size][D]; page_table [batch][max_pages] int32; cache_lens [batch] int32.  The tensors
+    stay the caller's: new pages are handed out by writing page_table."""
+
+    def __init__(self, p: PagedParams, k_pages, v_pages, page_table, cache_lens):
+        self.p = p
+        self.dtype = torch.bfloat16 if p.dtype == BF16 else torch.float32
+        self.device = k_pages.device
+        pages = (p.n_pages, p.n_kv_heads, p.page_size, p.head_dim)
+        self._fits(k_pages, "k_pages", self.dtype, pages)
+        self._fits(v_pages, "v_pages", self.dtype, pages)
+        self._fits(page_table, "page_table", torch.int32, (p.batch, p.max_pages))
+        self._fits(cache_lens, "cache_lens", torch.int32, (p.batch,))
+        self.k_pages, self.v_pages, self.page_table, self.cache_lens = k_pages, v_pages, page_table, cache_lens
+        self.workspace = None
+
+    def _fits(self, t, name: str, dtype, shape) -> None:
+        if t.shape != shape or t.dtype != dtype or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{name}: {dtype} {list(shape)} on {self.device}, contiguous, expected, not {t.dtype} "
+                             f"{list(t.shape)} on {t.device} with strides {list(t.stride())}")
+
+    def _on_device(self, stream) -> Optional[int]:
+        if self.device.type != "cuda" or self.device.index != _raw_device():
+            raise ValueError(f"the cache is on {self.device}, which is not the current device")
+        return _stream(stream)
+
+    def _heads(self, t, name: str, total: int, heads: int) -> int:
+        """Elements between the tokens of q, k or v [total][heads][D]: its heads follow one another, its tokens need not."""
+        d = self.p.head_dim
+        if t.shape != (total, heads, d) or t.dtype != self.dtype or t.device != self.device:
+            raise ValueError(f"{name}: {self.dtype} {[total, heads, d]} on {self.device} expected, not {t.dtype} {list(t.shape)} on {t.device}")
+        stride = t.stride()
+        if stride[2] != 1 or (stride[1] != d and heads > 1):
+            raise ValueError(f"{name}: the heads of a token have to follow one another (strides {list(stride)})")
+        return stride[0] if total > 1 else heads * d
+
+    def reserve(self, total_q: int, max_q_len: int, max_cache_len: int, shared_len: int = 0) -> None:
+        """A workspace for attention calls of up to these sizes.  Calls that overlap in time (two streams, two captured graphs)
+        need a PagedCache, and with it a workspace, each."""
+        if shared_len:
+            n = calidrop_paged_attend_shared_workspace_bytes(self.p, total_q, max_q_len, max_cache_len, shared_len)
+        else:
+            n = calidrop_paged_attend_workspace_bytes(self.p, total_q, max_q_len, max_cache_len)
+        if self.workspace is None or self.workspace.nbytes < n:
+            self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
+
+    def append(self, k, v, q=None, q_out=None, new_offsets=None, max_new: int = 1, positions=None, rot_table=None, new_lens=None,
+               stream=None) -> None:
+        """k, v [total][Hkv][D] become the next rows of the sequences, rotated on the way; q [total][Hq][D] goes rotated to q_out.
+        new_lens None: cache_lens grows in place."""
+        p, total = self.p, k.shape[0]
+        ks = self._heads(k, "k", total, p.n_kv_heads)
+        vs = self._heads(v, "v", total, p.n_kv_heads)
+        qs = 0
+        if (q is None) != (q_out is None):
+            raise ValueError("q and q_out go together")
+        if q is not None:
+            qs = self._heads(q, "q", total, p.n_q_heads)
+            self._fits(q_out, "q_out", self.dtype, (total, p.n_q_heads, p.head_dim))
+        if new_offsets is not None:
+            self._fits(new_offsets, "new_offsets", torch.int32, (p.batch + 1,))
+        if positions is not None:
+            self._fits(positions, "positions", torch.int32, (total,))
+        n_positions = 0
+        if p.rot_dim and rot_table is not None:
+            n_positions = rot_table.shape[0]
+            self._fits(rot_table, "rot_table", torch.float32, (n_positions, p.rot_dim))
+        if new_lens is None:
+            new_lens = self.cache_lens
+        else:
+            self._fits(new_lens, "new_lens", torch.int32, (p.batch,))
+        calidrop_paged_append(p, q, qs, k, ks, v, vs, new_offsets, total, max_new, positions, rot_table if p.rot_dim else None,
+                              n_positions, self.k_pages, self.v_pages, self.page_table, self.cache_lens, new_lens, q_out,
+                              self._on_device(stream))
+
+    def _queries(self, q, out, lse, q_offsets):
+        p, total = self.p, q.shape[0]
+        shape = (total, p.n_q_heads, p.head_dim)
+        self._fits(q, "q", self.dtype, shape)
+        self._fits(out, "out", self.dtype, shape)
+        self._fits(lse, "lse", torch.float32, shape[:2])
+        if q_offsets is not None:
+            self._fits(q_offsets, "q_offsets", torch.int32, (p.batch + 1,))
+        return total
+
+    def attend(self, q, out, lse, q_offsets=None, max_q_len: int = 1, max_cache_len: Optional[int] = None, stream=None) -> None:
+        """Attention of the newest tokens, q [total][Hq][D], over the cache, into out and lse [total][Hq]."""
+        total = self._queries(q, out, lse, q_offsets)
+        if max_cache_len is None:
+            max_cache_len = self.p.max_pages * self.p.page_size
+        calidrop_paged_attend(self.p, q, q_offsets, total, max_q_len, self.k_pages, self.v_pages, self.page_table, self.cache_lens,
+                              max_cache_len, out, lse, self.workspace, self._on_device(stream))
+
+    def attend_shared(self, q, out, lse, shared_table, shared_len: int, q_offsets=None, max_q_len: int = 1,
+                      max_cache_len: Optional[int] = None, stream=None) -> None:
+        """The same behind a prefix of shared_len rows in the pages shared_table."""
+        total = self._queries(q, out, lse, q_offsets)
+        if max_cache_len is None:
+            max_cache_len = self.p.max_pages * self.p.page_size
+        self._fits(shared_table, "shared_table", torch.int32, (-(-shared_len // self.p.page_size),))
+        calidrop_paged_attend_shared(self.p, q, q_offsets, total, max_q_len, self.k_pages, self.v_pages, shared_table, shared_len,
+                                     self.page_table, self.cache_lens, max_cache_len, out, lse, self.workspace,
+                                     self._on_device(stream))
 
 
 # ---- device-memory plumbing (allocation only) ----------------------------------------------

@@ -15,6 +15,7 @@
 #include "cd_common.h"
 #include "cd_given.h"
 #include "cd_h2o.h"
+#include "cd_paged.h"
 #include "cd_score.h"
 #include "cd_select.h"
 
@@ -1485,3 +1486,5 @@ int calidrop_append(const calidrop_params* p_in, const void* k_new, const void* 
 }
 
 }  // extern "C"
+
+#include "paged_calls.h"

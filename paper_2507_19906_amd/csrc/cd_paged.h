@@ -1,0 +1,485 @@
+// Keys and values in pages: appending new rows (with the position rotation applied on the way) and attention that reads
+// them - prompts, chunks of prompts and single tokens, whole contexts or a sliding window with a few first tokens that stay
+// visible, with or without a prefix that all sequences share.
+//
+// A page holds page_size rows of every KV head, [Hkv][page_size][D]: the layout of a prompt or compressed cache of that many
+// rows.  Row r of sequence b is row r % page_size of page table[b][r / page_size].
+#pragma once
+#include "cd_common.h"
+
+namespace cd {
+
+// ---- where a row is ---------------------------------------------------------------------------------------------------
+
+// x / d for 0 <= x < 2^31 as one 64-bit product and shift: magic = ceil(2^shift / d), shift = 31 + ceil(log2 d).  magic < 2^32
+// and x * (magic * d - 2^shift) < 2^31 * d <= 2^shift, so the quotient is exact.
+struct PageDiv { uint32_t magic; int shift; };
+__device__ __forceinline__ int page_div(int x, PageDiv d) {
+  return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(x)) * d.magic) >> d.shift);
+}
+
+struct Pages {
+  const int32_t* table;      // entries of sequence b at table + b * table_stride
+  int64_t table_stride;
+  int page_size, n_pages, Hkv;
+  PageDiv div;
+};
+
+// Row `pos` of KV head g as a row number of the page buffers (rows of D elements; below 2^32 for every buffer that fits the
+// card).  An entry that names no page is read as the nearest one that exists.
+__device__ __forceinline__ uint32_t page_row(const Pages& pg, const int32_t* table, int g, int pos) {
+  const int e = page_div(pos, pg.div);
+  const int page = min(max(table[e], 0), pg.n_pages - 1);
+  return (static_cast<uint32_t>(page) * pg.Hkv + g) * pg.page_size + (pos - e * pg.page_size);
+}
+
+// ---- append -------------------------------------------------------------------------------------------------------------
+
+struct PagedAppendArgs {
+  const char* q; const char* k; const char* v;      // [total][heads][D], tokens q_stride / k_stride / v_stride bytes apart
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t* new_off;                           // [batch+1] tokens of a sequence, or NULL: one each
+  const int32_t* positions;                         // [total] place in the text, or NULL: the row in the cache
+  const float* rot_table;                           // [n_positions][rot]: cosines, then sines
+  char* k_pages; char* v_pages; char* q_out;
+  const int32_t* lens; int32_t* new_lens;
+  Pages pages;
+  int64_t total_new;
+  int batch, Hq, max_new, max_pages, rot, n_positions, tokens_per_group, write_lens;
+};
+
+// 16 bytes of a row as 32-bit floats, and back.
+template <typename T> __device__ __forceinline__ void unpack16(const u32x4& x, float (&f)[Elem<T>::kPer16B]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t u = x[e];
+    if constexpr (sizeof(T) == 2) {
+      f[2 * e] = as_f32(u << 16);
+      f[2 * e + 1] = as_f32(u & 0xffff0000u);
+    } else {
+      f[e] = as_f32(u);
+    }
+  }
+}
+template <typename T> __device__ __forceinline__ u32x4 pack16(const float (&f)[Elem<T>::kPer16B]) {
+  u32x4 x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (sizeof(T) == 2) x[e] = pack_bf16x2(f[2 * e], f[2 * e + 1]);
+    else x[e] = __builtin_bit_cast(uint32_t, f[e]);
+  }
+  return x;
+}
+template <int N> __device__ __forceinline__ void load_floats(const float* p, float (&f)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; e += 4) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(p + e);
+    f[e] = x[0]; f[e + 1] = x[1]; f[e + 2] = x[2]; f[e + 3] = x[3];
+  }
+}
+
+// A workgroup takes tokens_per_group tokens of one sequence; a thread 16 bytes of one head (two pieces of 16 bytes, the two
+// elements of its pairs, where those lie half the rotated part apart).  The rotation is in 32 bits, rounded once to the
+// storage type.  Bound by the bytes of the heads, read and written once.
+template <typename T, int D, bool kHalves>
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
+  constexpr int E = Elem<T>::kPer16B;
+  constexpr int kChunks = D / E;
+  const int b = blockIdx.y;
+  int64_t t0 = b, t1 = b + 1;
+  if (a.new_off) { t0 = a.new_off[b]; t1 = a.new_off[b + 1]; }
+  t0 = min(max(t0, static_cast<int64_t>(0)), a.total_new);
+  t1 = min(max(t1, t0), a.total_new);
+  const int n = static_cast<int>(min(t1 - t0, static_cast<int64_t>(a.max_new)));
+  const int len = a.lens[b];
+  const bool fits = len >= 0 && static_cast<int64_t>(len) + n <= static_cast<int64_t>(a.max_pages) * a.pages.page_size;
+  const int first = static_cast<int>(blockIdx.x) * a.tokens_per_group;
+  __syncthreads();                                  // everyone has read the length before it changes
+  if (a.write_lens && blockIdx.x == 0 && threadIdx.x == 0) a.new_lens[b] = fits ? len + n : len;
+  const int here = min(a.tokens_per_group, n - first);
+  if (here <= 0) return;
+  const int32_t* table = a.pages.table + b * a.pages.table_stride;
+  const int Hq = a.q ? a.Hq : 0, Hkv = a.pages.Hkv, rot = a.rot;
+  const int turned_units = kHalves ? (D - rot / 2) / E : kChunks;      // threads of a turned head: a pair of pieces, or a piece
+  const int turned = (Hq + Hkv) * turned_units, per_token = turned + Hkv * kChunks;
+  for (int item = threadIdx.x; item < here * per_token; item += 256) {
+    const int tt = item / per_token, r = item - tt * per_token;
+    const int t = first + tt;
+    const int64_t token = t0 + t;
+    const char* src; char* dst;
+    int u; bool turn = false;
+    if (r < turned) {
+      const int h = r / turned_units;
+      u = r - h * turned_units;
+      turn = u < (kHalves ? rot / 2 : rot) / E;
+      if (kHalves && !turn) u += rot / 2 / E;       // the pieces behind the pairs
+      if (h < Hq) {
+        src = a.q + token * a.q_stride + static_cast<int64_t>(h) * D * sizeof(T);
+        dst = a.q_out + (token * Hq + h) * D * sizeof(T);
+      } else {
+        src = a.k + token * a.k_stride + static_cast<int64_t>(h - Hq) * D * sizeof(T);
+        dst = a.k_pages;
+      }
+      if (h >= Hq) {
+        if (!fits) continue;
+        const int e = page_div(len + t, a.pages.div), page = table[e];
+        if (page < 0 || page >= a.pages.n_pages) continue;
+        dst += ((static_cast<int64_t>(page) * Hkv + (h - Hq)) * a.pages.page_size + (len + t - e * a.pages.page_size)) * D * sizeof(T);
+      }
+    } else {
+      const int h = (r - turned) / kChunks;
+      u = (r - turned) - h * kChunks;
+      if (!fits) continue;
+      const int e = page_div(len + t, a.pages.div), page = table[e];
+      if (page < 0 || page >= a.pages.n_pages) continue;
+      src = a.v + token * a.v_stride + static_cast<int64_t>(h) * D * sizeof(T);
+      dst = a.v_pages + ((static_cast<int64_t>(page) * Hkv + h) * a.pages.page_size + (len + t - e * a.pages.page_size)) * D * sizeof(T);
+    }
+    if (!turn) { st16(dst + u * 16, ld16(src + u * 16)); continue; }
+    const int pos = min(max(a.positions ? a.positions[token] : len + t, 0), a.n_positions - 1);
+    const float* cs = a.rot_table + static_cast<int64_t>(pos) * rot;
+    if constexpr (kHalves) {
+      const int far = rot / 2 * static_cast<int>(sizeof(T));
+      float x[E], y[E], c[E], s[E], p[E], q[E];
+      unpack16<T>(ld16(src + u * 16), x);
+      unpack16<T>(ld16(src + u * 16 + far), y);
+      load_floats(cs + u * E, c);
+      load_floats(cs + rot / 2 + u * E, s);
+#pragma unroll
+      for (int e = 0; e < E; ++e) { p[e] = x[e] * c[e] - y[e] * s[e]; q[e] = y[e] * c[e] + x[e] * s[e]; }
+      st16(dst + u * 16, pack16<T>(p));
+      st16(dst + u * 16 + far, pack16<T>(q));
+    } else {
+      float x[E], p[E];
+      unpack16<T>(ld16(src + u * 16), x);
+#pragma unroll
+      for (int e = 0; e < E / 2; ++e) {
+        const float c = cs[u * (E / 2) + e], s = cs[rot / 2 + u * (E / 2) + e];
+        p[2 * e] = x[2 * e] * c - x[2 * e + 1] * s;
+        p[2 * e + 1] = x[2 * e + 1] * c + x[2 * e] * s;
+      }
+      st16(dst + u * 16, pack16<T>(p));
+    }
+  }
+}
+
+// new_lens of calls whose sequences have several workgroups, where it is the array the lengths are read from.
+__global__ __launch_bounds__(256) void paged_lens_kernel(PagedAppendArgs a) {
+  const int b = blockIdx.x * 256 + threadIdx.x;
+  if (b >= a.batch) return;
+  int64_t t0 = min(max(static_cast<int64_t>(a.new_off[b]), static_cast<int64_t>(0)), a.total_new);
+  int64_t t1 = min(max(static_cast<int64_t>(a.new_off[b + 1]), t0), a.total_new);
+  const int n = static_cast<int>(min(t1 - t0, static_cast<int64_t>(a.max_new)));
+  const int len = a.lens[b];
+  const bool fits = len >= 0 && static_cast<int64_t>(len) + n <= static_cast<int64_t>(a.max_pages) * a.pages.page_size;
+  a.new_lens[b] = fits ? len + n : len;
+}
+
+// ---- attention ------------------------------------------------------------------------------------------------------------
+
+struct PagedAttendArgs {
+  const void* q;             // [total_q][Hq][D]
+  const int32_t* q_off;      // [batch+1], or NULL: one token each
+  const void* k; const void* v;
+  const int32_t* lens;       // rows of each sequence's cache, or NULL: fixed_len rows
+  Pages pages;
+  int fixed_len, max_len;
+  int64_t total_q;
+  int batch, Hq, G, max_q_len;
+  int window, sinks;         // window 0: no limit
+  int all_see_all;           // a prefix: every query sees every row
+  float sl2;                 // scale * log2(e)
+  void* out; float* lse;     // one split: the results
+  float* part_o;             // several: [total_q][Hq][slots][D] unnormalised outputs
+  float2* part_ml;           // [total_q][Hq][slots] (maximum in log2 units, sum)
+  int NS, tiles_per_split;   // splits of this launch, tiles of one
+  int slots, slot0;          // partials of a row, and the first of this launch
+};
+
+// The tokens of sequence b: first token and number.
+__device__ __forceinline__ int query_range(const PagedAttendArgs& a, int b, int64_t& q0) {
+  if (a.all_see_all) { q0 = 0; return static_cast<int>(a.total_q); }
+  int64_t q1;
+  if (a.q_off) { q0 = a.q_off[b]; q1 = a.q_off[b + 1]; } else { q0 = b; q1 = b + 1; }
+  q0 = min(max(q0, static_cast<int64_t>(0)), a.total_q);
+  q1 = min(max(q1, q0), a.total_q);
+  return static_cast<int>(min(q1 - q0, static_cast<int64_t>(a.max_q_len)));
+}
+__device__ __forceinline__ int cache_rows(const PagedAttendArgs& a, int b) {
+  return a.lens ? min(max(a.lens[b], 0), a.max_len) : a.fixed_len;
+}
+
+// The tiles of TK rows that a block of queries needs: those that hold one of the first `sinks` rows, then those from the
+// oldest query's window to the newest query.  A tile takes part with the rows of its range only, so that a tile of both
+// ranges counts no row twice, and rows outside (freed pages, rows behind the end) are never read.
+template <int TK>
+struct KeyTiles {
+  int n_sink, n, first, sink_end, lo, hi;
+  __device__ __forceinline__ KeyTiles(int len, int pos_min, int pos_max, int window, int sinks) {
+    hi = min(len, pos_max + 1);
+    lo = window ? max(0, pos_min - window + 1) : 0;
+    sink_end = window ? min(sinks, hi) : 0;
+    if (lo <= sink_end) { lo = 0; sink_end = 0; }      // one range
+    n_sink = (sink_end + TK - 1) / TK;
+    first = lo / TK;
+    n = hi > 0 ? n_sink + (hi + TK - 1) / TK - first : 0;
+  }
+  __device__ __forceinline__ void tile(int u, int& base, int& from, int& to) const {
+    const bool s = u < n_sink;
+    base = (s ? u : first + u - n_sink) * TK;
+    from = s ? 0 : lo;
+    to = s ? sink_end : hi;
+  }
+};
+
+// Few queries: a workgroup owns the queries of one (sequence, KV head) - up to 16 NT (token, head) rows of its group - and a
+// stretch of the cache; its 4 waves take 32-row tiles in turn.  S^T = K Q^T on the matrix cores puts a query into a column,
+// so that its softmax weights stay in the lanes that made them and are the B operand of O^T += V^T P^T as they are: the rows
+// of a tile are dealt to the K operand in the order in which the products want the weights.  K and V go from memory to
+// registers without LDS.  Bound by the bytes of K and V.
+template <typename T, int D, int NT>
+struct PagedWave {
+  static constexpr int EPL = Elem<T>::kPer16B, KD = Elem<T>::kStepK, NK = D / KD;
+  static constexpr bool kBf16 = sizeof(T) == 2;
+  static constexpr int NP = kBf16 ? 1 : D / 64;            // 16-byte pieces of a V row per lane (bf16, D = 64: 8 bytes)
+  static constexpr int NX = kBf16 ? D / 16 : 4;            // elements of a piece
+  static constexpr int NACC = NP * NX;                     // O^T tiles: 16 rows (slots of D) x 16 queries
+  typedef uint32_t VPiece __attribute__((ext_vector_type(kBf16 && D == 64 ? 2 : 4)));
+
+  u32x4 qf[NT][NK];
+  f32x4 o[NT][NACC];
+  float m[NT], l[NT];                                      // running maximum (log2 units) and this lane's share of the sum
+
+  // row of a tile that lane (i, c) loads for K group t, and for slot e of V
+  static __device__ __forceinline__ int k_row(int t, int i) { return kBf16 ? 8 * (i >> 2) + 4 * t + (i & 3) : 16 * t + i; }
+  static __device__ __forceinline__ int v_row(int e, int c) { return kBf16 ? 8 * c + e : 16 * (e >> 2) + 4 * c + (e & 3); }
+  // row of a tile of weight r of K group t in lane group c
+  static __device__ __forceinline__ int p_row(int t, int c, int r) { return kBf16 ? 8 * c + 4 * t + r : 16 * t + 4 * c + r; }
+  // first of the elements of D that lane group c holds of output piece p: o[.][p NX + x][r] is element d_first + r NX + x
+  static __device__ __forceinline__ int d_first(int p, int c) { return p * 64 + c * 4 * NX; }
+
+  __device__ __forceinline__ void load_k(const T* k, uint32_t rid, int i, int c, u32x4 (&kf)[2][NK]) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const T* kp = k + static_cast<int64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(rid), k_row(t, i)))) * D + c * EPL;
+#pragma unroll
+      for (int kk = 0; kk < NK; ++kk) kf[t][kk] = ld16_stream(kp + kk * KD);
+    }
+  }
+  __device__ __forceinline__ void load_v(const T* v, uint32_t rid, int i, int c, VPiece (&vf)[8][NP]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const T* vp = v + static_cast<int64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(rid), v_row(e, c)))) * D + i * NX;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) vf[e][p] = __builtin_nontemporal_load(reinterpret_cast<const VPiece*>(vp + p * 64));
+    }
+  }
+  // A operand of output tile (p, x): slot i holds element p 64 + i NX + x of the rows of lane group c
+  __device__ __forceinline__ u32x4 v_operand(const VPiece (&vf)[8][NP], int p, int x, int t) const {
+    u32x4 f;
+    if constexpr (kBf16) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t lo = vf[2 * j][0][x >> 1], hi = vf[2 * j + 1][0][x >> 1];
+        f[j] = __builtin_amdgcn_perm(hi, lo, x & 1 ? 0x07060302u : 0x05040100u);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = vf[4 * t + j][p][x];
+    }
+    return f;
+  }
+};
+
+template <typename T, int D, int NT>
+__global__ __launch_bounds__(256) void paged_stream_kernel(PagedAttendArgs a) {
+  using W = PagedWave<T, D, NT>;
+  constexpr int TK = 32, kWaves = 4;
+  const int rb = blockIdx.x / a.NS, split = blockIdx.x - rb * a.NS, g = blockIdx.y, b = blockIdx.z;
+  const int lane = threadIdx.x & 63, i = lane & 15, c = lane >> 4, wave = wave_index();
+  int64_t q0;
+  const int nq = query_range(a, b, q0), R = nq * a.G, r0 = rb * 16 * NT;
+  if (r0 >= R) return;
+  const int len = cache_rows(a, b);
+  const int past = len - nq;
+  const int pos_min = a.all_see_all ? len - 1 : past + r0 / a.G;
+  const int pos_max = a.all_see_all ? len - 1 : past + (min(r0 + 16 * NT, R) - 1) / a.G;
+  const KeyTiles<TK> kt(len, pos_min, pos_max, a.window, a.sinks);
+  const int u_end = min(kt.n, (split + 1) * a.tiles_per_split);
+  const int32_t* table = a.pages.table + b * a.pages.table_stride;
+  const T* K = static_cast<const T*>(a.k);
+  const T* V = static_cast<const T*>(a.v);
+
+  W w;
+  int64_t row[NT];                                         // (token, head) of this lane's column, -1: none
+  int pos[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = r0 + 16 * nt + i;
+    const bool valid = r < R;
+    const int t = valid ? r / a.G : 0;
+    row[nt] = valid ? (q0 + t) * a.Hq + g * a.G + (r - t * a.G) : -1;
+    pos[nt] = !valid ? -1 : a.all_see_all ? len - 1 : past + t;
+    const T* qp = static_cast<const T*>(a.q) + (valid ? row[nt] : 0) * D + c * W::EPL;
+#pragma unroll
+    for (int kk = 0; kk < W::NK; ++kk) w.qf[nt][kk] = valid ? ld16(qp + kk * W::KD) : zero16();
+#pragma unroll
+    for (int x = 0; x < W::NACC; ++x) w.o[nt][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    w.m[nt] = -INFINITY;
+    w.l[nt] = 0.f;
+  }
+  auto row_of = [&](int u) -> uint32_t {                   // of row lane % 32 of the tile
+    int base, from, to;
+    kt.tile(u, base, from, to);
+    return page_row(a.pages, table, g, min(max(base + (lane & 31), from), to - 1));
+  };
+  int u = split * a.tiles_per_split + wave;
+  uint32_t rid = u < u_end ? row_of(u) : 0;
+  while (u < u_end) {
+    u32x4 kf[2][W::NK];
+    typename W::VPiece vf[8][W::NP];
+    w.load_k(K, rid, i, c, kf);
+    w.load_v(V, rid, i, c, vf);
+    int base, from, to;
+    kt.tile(u, base, from, to);
+    u += kWaves;
+    if (u < u_end) rid = row_of(u);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int kk = 0; kk < W::NK; ++kk)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) mma_step<T>(s[t], kf[t][kk], w.qf[nt][kk]);
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int j = base + W::p_row(t, c, r);
+          const bool see = j >= from && j < to && j <= pos[nt] && (a.window == 0 || j > pos[nt] - a.window || j < a.sinks);
+          s[t][r] = see ? s[t][r] * a.sl2 : -INFINITY;
+          top = fmaxf(top, s[t][r]);
+        }
+      const float mn = fmaxf(w.m[nt], col4_max(top));
+      const float ref = mn == -INFINITY ? 0.f : mn;
+      const float f = mn == w.m[nt] ? 1.f : fast_exp2(w.m[nt] - ref);
+      w.m[nt] = mn;
+      float sum = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { s[t][r] = fast_exp2(s[t][r] - ref); sum += s[t][r]; }
+      w.l[nt] = w.l[nt] * f + sum;
+      if (__any(f != 1.f)) {
+#pragma unroll
+        for (int x = 0; x < W::NACC; ++x) w.o[nt][x] *= f;
+      }
+      // The weights are rounded to the type of V, the precision the matrix cores take them in.
+      if constexpr (W::kBf16) {
+        const u32x4 pf = {pack_bf16x2(s[0][0], s[0][1]), pack_bf16x2(s[0][2], s[0][3]), pack_bf16x2(s[1][0], s[1][1]), pack_bf16x2(s[1][2], s[1][3])};
+#pragma unroll
+        for (int x = 0; x < W::NX; ++x) mma_step<T>(w.o[nt][x], w.v_operand(vf, 0, x, 0), pf);
+      } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const u32x4 pf = __builtin_bit_cast(u32x4, s[t]);
+#pragma unroll
+          for (int p = 0; p < W::NP; ++p)
+#pragma unroll
+            for (int x = 0; x < W::NX; ++x) mma_step<T>(w.o[nt][p * W::NX + x], w.v_operand(vf, p, x, t), pf);
+        }
+      }
+    }
+  }
+
+  // The four waves' shares, joined pairwise through LDS: (2, 3) into (0, 1), then 1 into 0.
+  __shared__ f32x4 so[2][NT][W::NACC][64];
+  __shared__ float sm[2][NT][64], sl[2][NT][64];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) w.l[nt] = col4_sum(w.l[nt]);
+#pragma unroll
+  for (int half = 2; half >= 1; half >>= 1) {
+    if (wave >= half && wave < 2 * half) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int x = 0; x < W::NACC; ++x) so[wave - half][nt][x][lane] = w.o[nt][x];
+        sm[wave - half][nt][lane] = w.m[nt];
+        sl[wave - half][nt][lane] = w.l[nt];
+      }
+    }
+    __syncthreads();
+    if (wave < half) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float m2 = sm[wave][nt][lane], mn = fmaxf(w.m[nt], m2), ref = mn == -INFINITY ? 0.f : mn;
+        const float f = fast_exp2(w.m[nt] - ref), f2 = fast_exp2(m2 - ref);
+        w.m[nt] = mn;
+        w.l[nt] = w.l[nt] * f + sl[wave][nt][lane] * f2;
+#pragma unroll
+        for (int x = 0; x < W::NACC; ++x) w.o[nt][x] = w.o[nt][x] * f + so[wave][nt][x][lane] * f2;
+      }
+    }
+    __syncthreads();
+  }
+  if (wave != 0) return;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    if (row[nt] < 0) continue;
+    if (a.slots > 1) {
+      const int64_t at = row[nt] * a.slots + a.slot0 + split;
+      if (c == 0) a.part_ml[at] = float2{w.m[nt], w.l[nt]};
+      if (w.l[nt] == 0.f) continue;
+#pragma unroll
+      for (int p = 0; p < W::NP; ++p)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int x = 0; x < W::NX; ++x) a.part_o[at * D + W::d_first(p, c) + r * W::NX + x] = w.o[nt][p * W::NX + x][r];
+    } else {
+      const float inv = w.l[nt] > 0.f ? 1.f / w.l[nt] : 0.f;
+#pragma unroll
+      for (int p = 0; p < W::NP; ++p)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int x = 0; x < W::NX; ++x)
+            store_elem(static_cast<T*>(a.out), row[nt] * D + W::d_first(p, c) + r * W::NX + x, w.o[nt][p * W::NX + x][r] * inv);
+      if (c == 0) a.lse[row[nt]] = w.l[nt] > 0.f ? (w.m[nt] + fast_log2(w.l[nt])) * kLn2 : -INFINITY;
+    }
+  }
+}
+
+// The partial results of a (token, head) joined: one wave each.  Tokens that no sequence owns are left as they are.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttendArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + wave_index();
+  const int64_t q_first = a.q_off ? a.q_off[0] : 0, q_end = a.q_off ? min(static_cast<int64_t>(a.q_off[a.batch]), a.total_q) : a.total_q;
+  const int64_t token = row / a.Hq;
+  if (token < q_first || token >= q_end) return;
+  const float2* ml = a.part_ml + row * a.slots;
+  float top = -INFINITY;
+  for (int s = lane; s < a.slots; s += 64) top = fmaxf(top, ml[s].x);
+  top = fmaxf(top, __shfl_xor(top, 1)); top = fmaxf(top, __shfl_xor(top, 2)); top = fmaxf(top, __shfl_xor(top, 4));
+  top = fmaxf(top, __shfl_xor(top, 8)); top = fmaxf(top, __shfl_xor(top, 16)); top = fmaxf(top, __shfl_xor(top, 32));
+  const float ref = top == -INFINITY ? 0.f : top;
+  constexpr int N = D / 64;
+  float o[N] = {}, l = 0.f;
+  for (int s = 0; s < a.slots; ++s) {
+    const float2 x = ml[s];
+    if (!(x.y > 0.f)) continue;
+    const float f = fast_exp2(x.x - ref);
+    l += x.y * f;
+    const float* po = a.part_o + (row * a.slots + s) * D + lane * N;
+#pragma unroll
+    for (int e = 0; e < N; ++e) o[e] += po[e] * f;
+  }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < N; ++e) store_elem(static_cast<T*>(a.out), row * D + lane * N + e, o[e] * inv);
+  if (lane == 0) a.lse[row] = l > 0.f ? (ref + fast_log2(l)) * kLn2 : -INFINITY;
+}
+
+}  // namespace cd
