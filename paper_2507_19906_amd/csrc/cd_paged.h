@@ -6,6 +6,7 @@
 // rows.  Row r of sequence b is row r % page_size of page table[b][r / page_size].
 #pragma once
 #include "cd_common.h"
+#include "cd_score.h"
 
 namespace cd {
 
@@ -448,6 +449,234 @@ __global__ __launch_bounds__(256) void paged_stream_kernel(PagedAttendArgs a) {
             store_elem(static_cast<T*>(a.out), row[nt] * D + W::d_first(p, c) + r * W::NX + x, w.o[nt][p * W::NX + x][r] * inv);
       if (c == 0) a.lse[row[nt]] = w.l[nt] > 0.f ? (w.m[nt] + fast_log2(w.l[nt])) * kLn2 : -INFINITY;
     }
+  }
+}
+
+// Many queries: the tiles of 64 rows go through LDS, where the 4 waves of a workgroup share them, 32 (token, head) rows of a
+// group to a wave.  The next tile is on its way (straight into LDS, two buffers) while one is worked on.
+//
+// S^T = K Q^T in products of 32 x 32 x 16: a lane has one query (l % 32) and of 32 rows the 16 rows 8 (r / 4) + 4 h + r % 4,
+// h = l / 32.  Its weights are the B operand of O^T += V^T P^T as they are, since the order of the contraction is free: step s
+// of 32 rows takes 16 s + 4 h + {0..3, 8..11} from lane half h.  V^T comes from LDS by transposing reads: 16 lanes name 4 rows
+// x 4 pieces of 4 elements (lane i: row i / 4, piece i % 4) and get a column of 4 each; which elements of D make up the pieces
+// is free too, and is taken so that a lane ends with 8 neighbouring elements of its query's output.  16-byte pieces of a row
+// are permuted by XOR with the row in LDS (K: row % 8, V: 2 (row % 4)), which makes both kinds of reads free of conflicts.
+//
+// Sums are taken against a reference that follows the maximum only when a tile exceeds it by 2^8 (any reference gives the
+// same result while nothing overflows), so that the outputs are rarely rescaled.
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+
+template <int D>
+struct PagedTile {
+  static constexpr int TK = 64, kRows = 128, kWaves = 4;
+  static constexpr int kRowBytes = 2 * D, kChunks = D / 8;         // 16-byte pieces of a row
+  static constexpr int kPerLoad = 64 / kChunks;                    // rows of one load instruction
+  static constexpr int kLoads = TK / kWaves / kPerLoad;
+  static constexpr int kTileBytes = TK * kRowBytes;
+  static constexpr int NS = D / 16, ND = D / 32;
+};
+
+__device__ __forceinline__ f32x16 mma32(const u32x4& a, const u32x4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
+  using P = PagedTile<D>;
+  constexpr int TK = P::TK;
+  __shared__ __attribute__((aligned(16))) char s_k[2][P::kTileBytes], s_v[2][P::kTileBytes];
+  // workgroups of a (sequence, KV head) behind one L2, the longest rows of a prompt first
+  int x, gb;
+  xcd_head_major(x, gb);
+  const int g = gb % a.pages.Hkv, b = gb / a.pages.Hkv;
+  const int blocks = static_cast<int>(gridDim.x) / a.NS;
+  const int split = x % a.NS, rb = blocks - 1 - x / a.NS;
+  const int lane = threadIdx.x & 63, wave = wave_index(), col = lane & 31, h = lane >> 5;
+  int64_t q0;
+  const int nq = query_range(a, b, q0), R = nq * a.G, r0 = rb * P::kRows;
+  if (r0 >= R) return;
+  const int len = cache_rows(a, b), past = len - nq;
+  const int pos_min = a.all_see_all ? len - 1 : past + r0 / a.G;
+  const int pos_max = a.all_see_all ? len - 1 : past + (min(r0 + P::kRows, R) - 1) / a.G;
+  const KeyTiles<TK> kt(len, pos_min, pos_max, a.window, a.sinks);
+  const int u0 = split * a.tiles_per_split, u_end = min(kt.n, u0 + a.tiles_per_split);
+
+  // this wave's rows
+  const int wr0 = r0 + 32 * wave, r = wr0 + col;
+  const bool valid = r < R, any_rows = wr0 < R;
+  const int t = valid ? r / a.G : 0;
+  const int64_t row = (q0 + t) * a.Hq + g * a.G + (r - t * a.G);       // where valid
+  const int pos = !valid ? -1 : a.all_see_all ? len - 1 : past + t;
+  const int wave_min = a.all_see_all ? len - 1 : past + wr0 / a.G;
+  const int wave_max = a.all_see_all ? len - 1 : past + (min(wr0 + 32, R) - 1) / a.G;
+  u32x4 qf[P::NS];
+#pragma unroll
+  for (int s = 0; s < P::NS; ++s)
+    qf[s] = valid ? ld16(static_cast<const uint16_t*>(a.q) + row * D + s * 16 + h * 8) : zero16();
+  f32x16 o[P::ND];
+#pragma unroll
+  for (int d = 0; d < P::ND; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+  float ref = -INFINITY, l = 0.f;                      // reference (unscaled logits), this lane's share of the sum
+
+  // a tile's rows on their way: this wave brings 16 of them, lane % 16 looks up the page of one
+  const int32_t* table = a.pages.table + b * a.pages.table_stride;
+  int entry = 0, at_row = 0;
+  auto look_up = [&](int u) {
+    int base, from, to;
+    kt.tile(u, base, from, to);
+    const int p = min(max(base + 16 * wave + (lane & 15), from), to - 1);
+    const int e = page_div(p, a.pages.div);
+    at_row = p - e * a.pages.page_size;
+    entry = table[e];
+  };
+  auto row_number = [&]() -> uint32_t {
+    const int page = min(max(entry, 0), a.pages.n_pages - 1);
+    return (static_cast<uint32_t>(page) * a.pages.Hkv + g) * a.pages.page_size + at_row;
+  };
+  const int sub = lane / P::kChunks, piece = lane % P::kChunks;
+  auto issue = [&](uint32_t rid, char* kd, char* vd) {
+#pragma unroll
+    for (int n = 0; n < P::kLoads; ++n) {
+      const int in_wave = n * P::kPerLoad + sub;                     // row of the wave's 16
+      const int64_t off = static_cast<int64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(rid), in_wave))) * D;
+      load_to_lds16(static_cast<const uint16_t*>(a.k) + off + ((piece ^ (in_wave & 7)) * 8), kd + (16 * wave + n * P::kPerLoad) * P::kRowBytes);
+      load_to_lds16(static_cast<const uint16_t*>(a.v) + off + ((piece ^ (2 * (in_wave & 3))) * 8), vd + (16 * wave + n * P::kPerLoad) * P::kRowBytes);
+    }
+  };
+
+  // offsets of this lane's reads
+  uint32_t k_off[4], v_off[2];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) k_off[s] = col * P::kRowBytes + (((2 * s) ^ (h ^ (lane & 7))) * 16);
+  const int li = lane & 15, dh = (lane >> 4) & 1;
+#pragma unroll
+  for (int d = 0; d < 2; ++d)
+    v_off[d] = (4 * h + (li >> 2)) * P::kRowBytes + (((4 * d) ^ (2 * dh + (li & 1)) ^ (2 * (li >> 2))) * 16) + ((li & 3) >> 1) * 8;
+
+  auto step = [&](int u, const char* __restrict kc, const char* __restrict vc, char* __restrict kn, char* __restrict vn) __attribute__((always_inline)) {
+    const bool more = u + 1 < u_end;
+    if (more) {
+      const uint32_t rid = row_number();
+      if (u + 2 < u_end) look_up(u + 2);
+      issue(rid, kn, vn);
+    }
+    int base, from, to;
+    kt.tile(u, base, from, to);
+    if (any_rows && base <= wave_max) {
+      f32x16 s[2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+#pragma unroll
+        for (int st = 0; st < P::NS; ++st) {
+          const u32x4 kf = *reinterpret_cast<const u32x4*>(kc + k_off[st & 3] + (st >> 2) * 128 + kb * 32 * P::kRowBytes);
+          s[kb] = mma32(kf, qf[st], s[kb]);
+        }
+      }
+      const bool full = base >= from && base + TK <= to && base + TK - 1 <= wave_min &&
+                        (a.window == 0 || base > wave_max - a.window || base + TK <= a.sinks);
+      if (!full) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int j = base + 32 * kb + 8 * (e >> 2) + 4 * h + (e & 3);
+            const bool see = j >= from && j < to && j <= pos && (a.window == 0 || j > pos - a.window || j < a.sinks);
+            if (!see) s[kb][e] = -INFINITY;
+          }
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
+      float lo, hi;
+      pair32(top, lo, hi);
+      top = fmaxf(lo, hi);
+      if (__any((top - ref) * a.sl2 > 8.f)) {          // -inf - -inf is no number and asks for nothing
+        const float mn = fmaxf(ref, top), f = mn == ref ? 1.f : fast_exp2((ref - mn) * a.sl2);
+        ref = mn;
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < P::ND; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[d][e] *= f;
+      }
+      const float shift = ref == -INFINITY ? 0.f : ref * a.sl2;
+      u32x4 pf[2][2];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) { s[kb][e] = fast_exp2(s[kb][e] * a.sl2 - shift); l += s[kb][e]; }
+        // rounded to bf16, what the matrix cores take
+#pragma unroll
+        for (int sh = 0; sh < 2; ++sh)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) pf[kb][sh][j] = pack_bf16x2(s[kb][8 * sh + 2 * j], s[kb][8 * sh + 2 * j + 1]);
+      }
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int sh = 0; sh < 2; ++sh)
+#pragma unroll
+          for (int d = 0; d < P::ND; ++d) {
+            const char* vp = vc + v_off[d & 1] + (d >> 1) * 128 + (32 * kb + 16 * sh) * P::kRowBytes;
+            typedef __attribute__((address_space(3))) s16x4* LdsPtr;
+            const s16x4 lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)vp);
+            const s16x4 hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(vp + 8 * P::kRowBytes));
+            typedef __attribute__((ext_vector_type(8))) short s16x8;
+            const s16x8 vf = __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7);
+            o[d] = mma32(__builtin_bit_cast(u32x4, vf), pf[kb][sh], o[d]);
+          }
+    }
+    stage_barrier();
+    asm volatile("" : "+v"(entry));                    // looked at behind the wait of the barrier only
+  };
+  if (u0 < u_end) {
+    look_up(u0);
+    const uint32_t rid = row_number();
+    if (u0 + 1 < u_end) look_up(u0 + 1);
+    issue(rid, s_k[0], s_v[0]);
+    stage_barrier();
+    asm volatile("" : "+v"(entry));
+    int u = u0;
+    for (; u + 1 < u_end; u += 2) {
+      step(u, s_k[0], s_v[0], s_k[1], s_v[1]);
+      step(u + 1, s_k[1], s_v[1], s_k[0], s_v[0]);
+    }
+    if (u < u_end) step(u, s_k[0], s_v[0], s_k[1], s_v[1]);
+  }
+  if (!valid) return;
+  float lo, hi;
+  pair32(l, lo, hi);
+  l = lo + hi;
+  const float m = ref * a.sl2;                           // log2 units
+  if (a.slots > 1) {
+    const int64_t at = row * a.slots + a.slot0 + split;
+    if (h == 0) a.part_ml[at] = float2{m, l};
+    if (l == 0.f) return;
+#pragma unroll
+    for (int d = 0; d < P::ND; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<f32x4*>(a.part_o + at * D + 32 * d + 16 * (e >> 3) + 8 * h + (e & 4)) = f32x4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
+  } else {
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    uint16_t* out = static_cast<uint16_t*>(a.out) + row * D;
+#pragma unroll
+    for (int d = 0; d < P::ND; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; e += 8) {
+        u32x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(o[d][e + 2 * j] * inv, o[d][e + 2 * j + 1] * inv);
+        st16(out + 32 * d + 2 * e + 8 * h, w);
+      }
+    if (h == 0) a.lse[row] = l > 0.f ? (m + fast_log2(l)) * kLn2 : -INFINITY;
   }
 }
 

@@ -65,46 +65,58 @@ cd::Pages pages_of(const calidrop_paged_params* p, const int32_t* table, int64_t
 }
 
 // How an attention launch is cut up: rows (token, head of the group) of a workgroup, splits of the cache, tiles of a split.
+// Up to 32 rows stream the cache from memory to registers; more share tiles of it in LDS, in bf16 (fp32 products are sixteen
+// times slower than bf16 ones and wait for nothing).
 struct PagedPlan { int rows, NS, tiles; };
-constexpr int kPagedTile = 32;
-constexpr int kPagedWant = 2048;           // workgroups worth splitting for
+constexpr int kPagedTile = 32;             // rows of a streamed tile, half those of a shared one
+constexpr int kPagedRowsAtOnce = 65536;    // rows of all workgroups, up to which a call is split further
 constexpr int kPagedMostSplits = 128;
-constexpr int kPagedMostRows = 32;
+constexpr int kPagedMostRows = 128;
 
-// Tiles of the longest cache that the queries of a workgroup can see.
-int paged_tiles(const calidrop_paged_params* p, int64_t max_q_len, int64_t max_len) {
-  int64_t rows = max_len;
-  if (p->window) rows = std::min<int64_t>(rows, static_cast<int64_t>(p->window) + p->sinks + max_q_len + 2 * kPagedTile);
-  return static_cast<int>((rows + kPagedTile - 1) / kPagedTile);
+// Rows of the longest cache that the queries of a call can see.
+int64_t paged_rows_seen(const calidrop_paged_params* p, int64_t max_q_len, int64_t max_len) {
+  if (!p->window) return max_len;
+  return std::min<int64_t>(max_len, static_cast<int64_t>(p->window) + p->sinks + max_q_len);
 }
-int most_paged_splits(int tiles) { return std::max(1, std::min(kPagedMostSplits, ceil_div(tiles, 4))); }
+// Most tiles of `tile` rows that a workgroup of `rows` can need (cd::KeyTiles): under a window, the rows of the window and of the
+// sinks can begin and end inside a tile each, and share one.
+int64_t most_tiles(const calidrop_paged_params* p, int64_t q_len, int64_t max_len, int64_t rows, int64_t tile) {
+  const int64_t all = (max_len + tile - 1) / tile;
+  if (!p->window) return all;
+  const int64_t tokens = std::min(q_len, rows / (p->n_q_heads / p->n_kv_heads) + 2);
+  return std::min(all + 1, (p->window + tokens + tile - 1) / tile + 1 + (p->sinks + tile - 1) / tile);
+}
+int most_paged_splits(int64_t seen) { return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kPagedMostSplits, (seen + 127) / 128))); }
 
-PagedPlan plan_paged(const calidrop_paged_params* p, int64_t sequences, int64_t q_len, int64_t total_q, int tiles) {
+PagedPlan plan_paged(const calidrop_paged_params* p, int64_t sequences, int64_t q_len, int64_t total_q, int64_t max_len) {
   const int64_t G = p->n_q_heads / p->n_kv_heads, rows = q_len * G;
   PagedPlan plan;
-  plan.rows = rows <= 16 ? 16 : kPagedMostRows;
+  plan.rows = rows <= 16 ? 16 : rows <= 32 || p->dtype == CALIDROP_FP32 ? 32 : kPagedMostRows;
+  const bool shared = plan.rows == kPagedMostRows;
   const int64_t groups = p->n_kv_heads * std::max(sequences * ((rows + plan.rows - 1) / plan.rows), (total_q * G + plan.rows - 1) / plan.rows);
-  const int64_t want = std::min<int64_t>(most_paged_splits(tiles), kPagedWant / groups);
-  plan.NS = static_cast<int>(std::max<int64_t>(want, 1));
-  plan.tiles = std::max(4 * ceil_div(ceil_div(tiles, plan.NS), 4), 4);
-  plan.NS = std::max(1, ceil_div(tiles, plan.tiles));
+  const int64_t most = shared ? kPagedRowsAtOnce / plan.rows : 2048;
+  const int64_t want = std::max<int64_t>(std::min<int64_t>(most_paged_splits(paged_rows_seen(p, q_len, max_len)), most / groups), 1);
+  const int64_t tile = shared ? 2 * kPagedTile : kPagedTile, unit = shared ? 2 : 4;     // no fewer than 128 rows
+  const int64_t tiles = most_tiles(p, q_len, max_len, plan.rows, tile);
+  plan.tiles = static_cast<int>(std::max((((tiles + want - 1) / want) + unit - 1) / unit * unit, unit));
+  plan.NS = static_cast<int>(std::max<int64_t>(1, (tiles + plan.tiles - 1) / plan.tiles));
   return plan;
 }
 
-// Room for the partials of `rows` (token, head) rows: a call is split into kPagedWant workgroups of kPagedMostRows rows at most.
-size_t partial_rows(int64_t rows, int tiles) {
-  return static_cast<size_t>(std::min<int64_t>(rows * most_paged_splits(tiles), static_cast<int64_t>(kPagedWant) * kPagedMostRows));
+// Room for the partials of `rows` (token, head) rows: splits of a call make kPagedRowsAtOnce rows at most.
+size_t partial_rows(int64_t rows, int64_t seen) {
+  return static_cast<size_t>(std::min<int64_t>(rows * most_paged_splits(seen), kPagedRowsAtOnce));
 }
 size_t partial_bytes(const calidrop_paged_params* p, size_t rows) {
   return round256(rows * sizeof(float2)) + round256(rows * p->head_dim * sizeof(float));
 }
 size_t attend_bytes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len, int32_t max_cache_len) {
-  return std::max<size_t>(256, partial_bytes(p, partial_rows(total_q * p->n_q_heads, paged_tiles(p, max_q_len, max_cache_len))));
+  return std::max<size_t>(256, partial_bytes(p, partial_rows(total_q * p->n_q_heads, paged_rows_seen(p, max_q_len, max_cache_len))));
 }
 size_t shared_bytes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len, int32_t max_cache_len, int32_t shared_len) {
   const int64_t rows = total_q * p->n_q_heads;       // where a side is not split its partials are there all the same
-  return std::max<size_t>(256, partial_bytes(p, 2 * rows + partial_rows(rows, paged_tiles(p, max_q_len, max_cache_len)) +
-                                                    partial_rows(rows, ceil_div(shared_len, kPagedTile))));
+  return std::max<size_t>(256, partial_bytes(p, 2 * rows + partial_rows(rows, paged_rows_seen(p, max_q_len, max_cache_len)) +
+                                                    partial_rows(rows, shared_len)));
 }
 
 int check_attend_sizes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len, int32_t max_cache_len) {
@@ -132,6 +144,12 @@ template <typename T, int D>
 int launch_paged(const cd::PagedAttendArgs& a, const PagedPlan& plan, int64_t sequences, int64_t q_len, hipStream_t st) {
   const int64_t rows = q_len * a.G, blocks = (rows + plan.rows - 1) / plan.rows;
   const dim3 grid(static_cast<unsigned>(blocks * plan.NS), a.pages.Hkv, static_cast<unsigned>(sequences));
+  if constexpr (sizeof(T) == 2) {
+    if (plan.rows == kPagedMostRows) {
+      hipLaunchKernelGGL((cd::paged_tile_kernel<D>), grid, dim3(256), 0, st, a);
+      return launch_status("paged_attend");
+    }
+  }
   if (plan.rows == 16) hipLaunchKernelGGL((cd::paged_stream_kernel<T, D, 1>), grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL((cd::paged_stream_kernel<T, D, 2>), grid, dim3(256), 0, st, a);
   return launch_status("paged_attend");
@@ -141,9 +159,9 @@ int launch_paged(const cd::PagedAttendArgs& a, const PagedPlan& plan, int64_t se
 template <typename T, int D>
 int attend_impl(const calidrop_paged_params* p, cd::PagedAttendArgs a, int32_t max_cache_len, const int32_t* shared_table,
                 int32_t shared_len, char* ws, hipStream_t st) {
-  const PagedPlan own = plan_paged(p, p->batch, a.max_q_len, a.total_q, paged_tiles(p, a.max_q_len, max_cache_len));
+  const PagedPlan own = plan_paged(p, p->batch, a.max_q_len, a.total_q, max_cache_len);
   PagedPlan prefix{};
-  if (shared_table) prefix = plan_paged(p, 1, a.total_q, a.total_q, ceil_div(shared_len, kPagedTile));
+  if (shared_table) prefix = plan_paged(p, 1, a.total_q, a.total_q, shared_len);
   a.slots = own.NS + prefix.NS;
   a.part_ml = reinterpret_cast<float2*>(ws);
   a.part_o = reinterpret_cast<float*>(ws + round256(static_cast<size_t>(a.total_q) * a.Hq * a.slots * sizeof(float2)));

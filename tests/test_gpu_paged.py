@@ -142,7 +142,7 @@ def test_head_layouts_and_a_few_tokens(hq, hkv, dtype, d):
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
-@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 3), (7, 1), (32, 4), (33, 32), (100, 5), (64, 200), (500, 7), (2 ** 31 - 1, 2 ** 31 - 1)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 3), (7, 1), (32, 4), (33, 32), (100, 5), (64, 200), (500, 7), (97, 1), (90, 30), (190, 2), (2 ** 31 - 1, 2 ** 31 - 1)])
 def test_one_token_under_a_window(dtype, d, window, sinks):
     lens = [1, 5, 32, 33, 40, 100, 131, 132, 133, 260, 0]
     Setup(lens, [1] * 11, 8, 2, d, dtype, 16, window, sinks, one=True, seed=window % 97).run().check()
@@ -176,7 +176,7 @@ def test_chunks_behind_a_cache(dtype, d, page):
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
-@pytest.mark.parametrize("window,sinks", [(1, 0), (5, 2), (31, 0), (64, 4), (65, 70), (128, 33), (1000, 3)])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (5, 2), (31, 0), (64, 4), (65, 70), (128, 33), (1000, 3), (190, 2), (60, 1)])
 def test_prompts_and_chunks_under_a_window(dtype, d, window, sinks):
     Setup([300, 129, 400, 64, 50], [300, 129, 60, 10, 60], 6, 2, d, dtype, 16, window, sinks, seed=7).run().check()
 
