@@ -296,7 +296,9 @@ template <typename T, int D, int NT>
 __global__ __launch_bounds__(256) void paged_stream_kernel(PagedAttendArgs a) {
   using W = PagedWave<T, D, NT>;
   constexpr int TK = 32, kWaves = 4;
-  const int rb = blockIdx.x / a.NS, split = blockIdx.x - rb * a.NS, g = blockIdx.y, b = blockIdx.z;
+  // workgroups go to the XCDs in turn and the late splits of short caches are empty: the splits are rotated from head to head
+  const int rb = blockIdx.x / a.NS, g = blockIdx.y, b = blockIdx.z;
+  const int split = static_cast<int>((blockIdx.x - rb * a.NS + g + gridDim.y * b) % a.NS);
   const int lane = threadIdx.x & 63, i = lane & 15, c = lane >> 4, wave = wave_index();
   int64_t q0;
   const int nq = query_range(a, b, q0), R = nq * a.G, r0 = rb * 16 * NT;
@@ -486,9 +488,15 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
   using P = PagedTile<D>;
   constexpr int TK = P::TK;
   __shared__ __attribute__((aligned(16))) char s_k[2][P::kTileBytes], s_v[2][P::kTileBytes];
-  // workgroups of a (sequence, KV head) behind one L2, the longest rows of a prompt first
-  int x, gb;
-  xcd_head_major(x, gb);
+  // workgroups of a (sequence, KV head) behind one L2, the heads of every sequence spread over the XCDs; the longest rows of a
+  // prompt first
+  int x = blockIdx.x, gb = blockIdx.y + gridDim.y * blockIdx.z;
+  if ((gridDim.y * gridDim.z) % 8 == 0) {
+    const int64_t at = x + static_cast<int64_t>(gridDim.x) * gb;
+    const int64_t slot = at / 8;
+    x = static_cast<int>(slot % gridDim.x);
+    gb = static_cast<int>(slot / gridDim.x) * 8 + static_cast<int>(at % 8);
+  }
   const int g = gb % a.pages.Hkv, b = gb / a.pages.Hkv;
   const int blocks = static_cast<int>(gridDim.x) / a.NS;
   const int split = x % a.NS, rb = blocks - 1 - x / a.NS;
@@ -680,30 +688,72 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
   }
 }
 
-// The partial results of a (token, head) joined: one wave each.  Tokens that no sequence owns are left as they are.
-template <typename T, int D>
+// The partial results of a (token, head) joined, by W waves: 1 where a workgroup joins four rows, 4 where the rows are few and
+// their partials many.  A partial without any row has no output, only its (maximum, sum).  Tokens that no sequence owns are left
+// as they are.
+constexpr int kJoinSlots = 256;                            // most partials of a row
+
+template <typename T, int D, int W>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttendArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + wave_index();
+  constexpr int N = D / 64, NJ = kJoinSlots / 64, U = 4;
+  const int lane = threadIdx.x & 63, wave = wave_index(), part = wave % W;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * (4 / W) + wave / W;
   const int64_t q_first = a.q_off ? a.q_off[0] : 0, q_end = a.q_off ? min(static_cast<int64_t>(a.q_off[a.batch]), a.total_q) : a.total_q;
   const int64_t token = row / a.Hq;
-  if (token < q_first || token >= q_end) return;
-  const float2* ml = a.part_ml + row * a.slots;
+  const bool owned = token >= q_first && token < q_end;
+  if (W == 1 && !owned) return;
+  const float2* ml = a.part_ml + (owned ? row : 0) * a.slots;
+  float2 x[NJ];
   float top = -INFINITY;
-  for (int s = lane; s < a.slots; s += 64) top = fmaxf(top, ml[s].x);
-  top = fmaxf(top, __shfl_xor(top, 1)); top = fmaxf(top, __shfl_xor(top, 2)); top = fmaxf(top, __shfl_xor(top, 4));
-  top = fmaxf(top, __shfl_xor(top, 8)); top = fmaxf(top, __shfl_xor(top, 16)); top = fmaxf(top, __shfl_xor(top, 32));
-  const float ref = top == -INFINITY ? 0.f : top;
-  constexpr int N = D / 64;
-  float o[N] = {}, l = 0.f;
-  for (int s = 0; s < a.slots; ++s) {
-    const float2 x = ml[s];
-    if (!(x.y > 0.f)) continue;
-    const float f = fast_exp2(x.x - ref);
-    l += x.y * f;
-    const float* po = a.part_o + (row * a.slots + s) * D + lane * N;
 #pragma unroll
-    for (int e = 0; e < N; ++e) o[e] += po[e] * f;
+  for (int j = 0; j < NJ; ++j) {
+    x[j] = 64 * j + lane < a.slots ? ml[64 * j + lane] : float2{-INFINITY, 0.f};
+    top = fmaxf(top, x[j].x);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  const float ref = top == -INFINITY ? 0.f : top;
+  float l = 0.f, f[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    f[j] = x[j].y > 0.f ? fast_exp2(x[j].x - ref) : 0.f;
+    l += x[j].y * f[j];
+  }
+  l = wave_sum(l);
+  float o[N] = {};
+  const float* po = a.part_o + (owned ? row : 0) * a.slots * D + lane * N;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    if (64 * j >= a.slots) break;
+    for (int s = part; s < min(64, a.slots - 64 * j); s += W * U) {
+      float w[U];
+      bool any = false;
+#pragma unroll
+      for (int y = 0; y < U; ++y) {
+        w[y] = s + W * y < 64 ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f[j]), min(s + W * y, 63))) : 0.f;
+        any |= w[y] != 0.f;
+      }
+      if (!any) continue;
+      float v[U][N];
+#pragma unroll
+      for (int y = 0; y < U; ++y)
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[y][e] = w[y] != 0.f ? po[static_cast<int64_t>(64 * j + s + W * y) * D + e] : 0.f;
+#pragma unroll
+      for (int y = 0; y < U; ++y)
+#pragma unroll
+        for (int e = 0; e < N; ++e) o[e] += v[y][e] * w[y];
+    }
+  }
+  if constexpr (W > 1) {
+    __shared__ float so[W][D];
+#pragma unroll
+    for (int e = 0; e < N; ++e) so[part][lane * N + e] = o[e];
+    __syncthreads();
+    if (part != 0 || !owned) return;
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      for (int w = 1; w < W; ++w) o[e] += so[w][lane * N + e];
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll

@@ -175,8 +175,10 @@ int attend_impl(const calidrop_paged_params* p, cd::PagedAttendArgs a, int32_t m
   a.NS = own.NS; a.tiles_per_split = own.tiles;
   if ((rc = launch_paged<T, D>(a, own, p->batch, a.max_q_len, st))) return rc;
   if (a.slots == 1) return CALIDROP_OK;
+  static_assert(2 * kPagedMostSplits <= cd::kJoinSlots, "the joining waves hold every partial of a row");
   const int64_t rows = a.total_q * a.Hq;
-  hipLaunchKernelGGL((cd::paged_join_kernel<T, D>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, st, a);
+  if (a.slots <= 8) hipLaunchKernelGGL((cd::paged_join_kernel<T, D, 1>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((cd::paged_join_kernel<T, D, 4>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, st, a);
   return launch_status("paged_join");
 }
 
