@@ -177,6 +177,13 @@ __global__ __launch_bounds__(256) void paged_lens_kernel(PagedAppendArgs a) {
 }
 
 // ---- attention ------------------------------------------------------------------------------------------------------------
+//
+// The work of a call is made of blocks: the queries of one sequence and KV head, as (token, head of the group) rows, cut into
+// blocks of kRows rows.  A block needs the tiles of its cache that one of its queries sees.  Either every workgroup has a block,
+// or, where there are too few blocks or their caches differ too much, a fixed number of workgroups shares the tiles of all
+// blocks of a KV head evenly, in order: a workgroup's share may begin and end inside a block.  The lengths are known to the
+// device alone, so each workgroup adds them up for itself.  Results of parts of blocks go to the workspace and are joined by a
+// second launch.
 
 struct PagedAttendArgs {
   const void* q;             // [total_q][Hq][D]
@@ -190,11 +197,16 @@ struct PagedAttendArgs {
   int window, sinks;         // window 0: no limit
   int all_see_all;           // a prefix: every query sees every row
   float sl2;                 // scale * log2(e)
-  void* out; float* lse;     // one split: the results
-  float* part_o;             // several: [total_q][Hq][slots][D] unnormalised outputs
-  float2* part_ml;           // [total_q][Hq][slots] (maximum in log2 units, sum)
-  int NS, tiles_per_split;   // splits of this launch, tiles of one
-  int slots, slot0;          // partials of a row, and the first of this launch
+  void* out; float* lse;
+  int blocks, items;         // blocks of a sequence at most, of all sequences
+  int share;                 // workgroups that share the tiles of a KV head, 0: one per block
+  int least_tiles;           // of a share
+  int keep;                  // whole blocks go to the workspace too: they are joined with another launch's
+  int4* cut;                 // [items] how a block was cut: first and last workgroup, 1 if it is not the first one's first
+  float* part_o;             // [Hkv][share][2][kRows][D] the parts of the block a workgroup begins with, and of the one it ends with
+  float2* part_ml;           // [Hkv][share][2][kRows]    unnormalised outputs; (maximum in log2 units, sum)
+  float* whole_o;            // keep: [total_q][Hq][D]
+  float2* whole_ml;          //       [total_q][Hq]
 };
 
 // The tokens of sequence b: first token and number.
@@ -216,7 +228,7 @@ __device__ __forceinline__ int cache_rows(const PagedAttendArgs& a, int b) {
 template <int TK>
 struct KeyTiles {
   int n_sink, n, first, sink_end, lo, hi;
-  __device__ __forceinline__ KeyTiles(int len, int pos_min, int pos_max, int window, int sinks) {
+  __device__ __forceinline__ void init(int len, int pos_min, int pos_max, int window, int sinks) {
     hi = min(len, pos_max + 1);
     lo = window ? max(0, pos_min - window + 1) : 0;
     sink_end = window ? min(sinks, hi) : 0;
@@ -233,8 +245,144 @@ struct KeyTiles {
   }
 };
 
-// Few queries: a workgroup owns the queries of one (sequence, KV head) - up to 16 NT (token, head) rows of its group - and a
-// stretch of the cache; its 4 waves take 32-row tiles in turn.  S^T = K Q^T on the matrix cores puts a query into a column,
+template <int kRows, int TK>
+struct PagedBlock {
+  int b, nq, R, r0, len, past;
+  int64_t q0;
+  KeyTiles<TK> kt;
+  __device__ __forceinline__ void init(const PagedAttendArgs& a, int item) {
+    b = a.blocks == 1 ? item : item / a.blocks;
+    r0 = (item - b * a.blocks) * kRows;
+    nq = query_range(a, b, q0);
+    R = nq * a.G;
+    len = cache_rows(a, b);
+    past = len - nq;
+    kt.init(len, pos_of(a, r0), pos_of(a, min(r0 + kRows, R) - 1), a.window, a.sinks);
+  }
+  // the last row that block row r sees
+  __device__ __forceinline__ int pos_of(const PagedAttendArgs& a, int r) const { return a.all_see_all ? len - 1 : past + r / a.G; }
+  // tiles, 1 for a block whose queries see nothing, 0 where there is no such block
+  __device__ __forceinline__ uint32_t weight() const { return r0 < R ? max(kt.n, 1) : 0; }
+};
+
+// The tiles lo .. hi-1 of all blocks of KV head g are workgroup w's; they begin in block `item`, whose first tile is `start`.
+struct PagedShare { int lo, hi, start, total; int item, g, w, W; };      // tiles of a launch: below 2^31
+
+template <int kRows, int TK, bool kShare>
+__device__ __forceinline__ PagedShare paged_share(const PagedAttendArgs& a, uint32_t* scratch) {
+  PagedShare s;
+  const int Hkv = a.pages.Hkv, x = blockIdx.x;
+  PagedBlock<kRows, TK> blk;
+  s.lo = s.hi = s.start = s.w = s.W = 0;
+  if constexpr (!kShare) {
+    // blocks of a (sequence, KV head) behind one L2 and the heads of every sequence spread over the XCDs, which workgroups go
+    // to in turn; the longest blocks of a prompt first
+    const int heads = Hkv * a.batch;
+    int rb, gb;
+    if (heads % 8 == 0) { const int slot = x / 8; rb = slot % a.blocks; gb = slot / a.blocks * 8 + x % 8; }
+    else { rb = x % a.blocks; gb = x / a.blocks; }
+    s.g = gb % Hkv;
+    s.item = gb / Hkv * a.blocks + (a.blocks - 1 - rb);
+    blk.init(a, s.item);
+    s.hi = s.total = blk.weight();
+    return s;
+  }
+  // the tiles of all blocks added up: a thread has up to (items + 255) / 256 blocks in a row
+  const int tid = threadIdx.x, per = (a.items + 255) / 256, i0 = tid * per, i1 = min(i0 + per, a.items);
+  uint32_t mine = 0, before = 0;
+  if (a.items == 1) {
+    blk.init(a, 0);
+    s.total = blk.weight();
+  } else {
+    for (int it = i0; it < i1; ++it) { blk.init(a, it); mine += blk.weight(); }
+    const uint32_t upto = wave_inclusive_scan(mine);
+    if ((tid & 63) == 63) scratch[tid >> 6] = upto;
+    __syncthreads();
+    const uint32_t t0 = scratch[0], t1 = scratch[1], t2 = scratch[2], t3 = scratch[3];
+    before = upto - mine + (tid >= 64 ? t0 : 0) + (tid >= 128 ? t1 : 0) + (tid >= 192 ? t2 : 0);
+    s.total = __builtin_amdgcn_readfirstlane(t0 + t1 + t2 + t3);
+  }
+  s.W = static_cast<int>(min(max(static_cast<uint32_t>(s.total) / a.least_tiles, 1u), static_cast<uint32_t>(a.share)));
+  s.item = 0;
+  if (s.W == a.share && 8 % Hkv == 0 && a.share % (8 / Hkv) == 0) {      // neighbouring shares behind one L2
+    const int xcd = x % 8;
+    s.g = xcd % Hkv;
+    s.w = xcd / Hkv * (a.share / (8 / Hkv)) + x / 8;
+  } else {
+    s.g = x % Hkv;
+    s.w = x / Hkv;
+  }
+  if (s.w >= s.W) return s;
+  s.lo = static_cast<int64_t>(s.total) * s.w / s.W;
+  s.hi = static_cast<int64_t>(s.total) * (s.w + 1) / s.W;
+  if (a.items > 1) {
+    if (before <= static_cast<uint32_t>(s.lo) && static_cast<uint32_t>(s.lo) < before + mine) {
+      uint32_t at = before;
+      int it = i0;
+      if (per > 1)
+        for (; it < i1; ++it) {
+          blk.init(a, it);
+          if (static_cast<uint32_t>(s.lo) < at + blk.weight()) break;
+          at += blk.weight();
+        }
+      scratch[4] = it;
+      scratch[5] = at;
+    }
+    __syncthreads();
+    s.item = __builtin_amdgcn_readfirstlane(scratch[4]);
+    s.start = __builtin_amdgcn_readfirstlane(scratch[5]);
+    __syncthreads();
+  }
+  return s;
+}
+
+// Where the results of workgroup rows go: out and lse, the whole rows' partials, or a part's.
+struct PagedTarget {
+  bool final_rows, by_row;
+  float* o; float2* ml;
+};
+// `begins`: the block is the first of the workgroup's.
+template <int kRows, int D, bool kShare, int TK>
+__device__ __forceinline__ PagedTarget paged_target(const PagedAttendArgs& a, const PagedShare& s, const PagedBlock<kRows, TK>& blk, int u0, int u1,
+                                                    bool begins) {
+  const int n = static_cast<int>(blk.weight());
+  if constexpr (!kShare) return PagedTarget{!a.keep, true, a.whole_o, a.whole_ml};
+  if (s.g == 0 && u0 == 0 && threadIdx.x == 0) {
+    // the last workgroup whose share begins ahead of the block's end
+    const int last = static_cast<int>((static_cast<int64_t>(s.start + n) * s.W + s.total - 1) / s.total) - 1;
+    a.cut[s.item] = int4{s.w, last, begins ? 0 : 1, 0};
+  }
+  if (u0 == 0 && u1 == n) return PagedTarget{!a.keep, true, a.whole_o, a.whole_ml};
+  const int64_t slot = (static_cast<int64_t>(s.g) * a.share + s.w) * 2 + (begins ? 0 : 1);
+  return PagedTarget{false, false, a.part_o + slot * kRows * D, a.part_ml + slot * kRows};
+}
+
+// f(block, u0, u1, first of the share) for every block that the workgroup has tiles u0 .. u1-1 of.
+template <int kRows, int TK, bool kShare, typename F>
+__device__ __forceinline__ void paged_blocks(const PagedAttendArgs& a, PagedShare& s, F&& f) {
+  if constexpr (!kShare) {
+    PagedBlock<kRows, TK> blk;
+    blk.init(a, s.item);
+    if (s.hi > 0) f(blk, 0, s.hi, true);
+    return;
+  }
+  bool begins = true;
+  while (s.lo < s.hi) {
+    PagedBlock<kRows, TK> blk;
+    blk.init(a, s.item);
+    const int n = static_cast<int>(blk.weight());
+    if (n > 0) {
+      const int u0 = s.lo - s.start, u1 = min(n, s.hi - s.start);
+      f(blk, u0, u1, begins);
+      begins = false;
+      s.lo = s.start + u1;
+    }
+    s.start += n;
+    ++s.item;
+  }
+}
+
+// Few queries, up to 16 (token, head) rows: the 4 waves of a workgroup take its 32-row tiles in turn.  S^T = K Q^T on the matrix cores puts a query into a column,
 // so that its softmax weights stay in the lanes that made them and are the B operand of O^T += V^T P^T as they are: the rows
 // of a tile are dealt to the K operand in the order in which the products want the weights.  K and V go from memory to
 // registers without LDS.  Bound by the bytes of K and V.
@@ -258,6 +406,75 @@ struct PagedWave {
   static __device__ __forceinline__ int p_row(int t, int c, int r) { return kBf16 ? 8 * c + 4 * t + r : 16 * t + 4 * c + r; }
   // first of the elements of D that lane group c holds of output piece p: o[.][p NX + x][r] is element d_first + r NX + x
   static __device__ __forceinline__ int d_first(int p, int c) { return p * 64 + c * 4 * NX; }
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int x = 0; x < NACC; ++x) o[nt][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m[nt] = -INFINITY;
+      l[nt] = 0.f;
+    }
+  }
+  __device__ __forceinline__ void load_q(int nt, const T* q, bool valid, int c) {
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) qf[nt][kk] = valid ? ld16(q + kk * KD + c * EPL) : zero16();
+  }
+  // Logits to weights: s[x] are those of K group t0 + x of the tile at `base`; sums and outputs so far are rescaled to the new
+  // maximum.
+  template <int N>
+  __device__ __forceinline__ void weigh(int nt, f32x4* s, int t0, int base, int from, int to, int pos, const PagedAttendArgs& a, int c) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int j = base + p_row(t0 + t, c, r);
+        const bool see = j >= from && j < to && j <= pos && (a.window == 0 || j > pos - a.window || j < a.sinks);
+        s[t][r] = see ? s[t][r] * a.sl2 : -INFINITY;
+        top = fmaxf(top, s[t][r]);
+      }
+    const float mn = fmaxf(m[nt], col4_max(top));
+    const float ref = mn == -INFINITY ? 0.f : mn;
+    const float f = mn == m[nt] ? 1.f : fast_exp2(m[nt] - ref);
+    m[nt] = mn;
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) { s[t][r] = fast_exp2(s[t][r] - ref); sum += s[t][r]; }
+    l[nt] = l[nt] * f + sum;
+    if (__any(f != 1.f)) {
+#pragma unroll
+      for (int x = 0; x < NACC; ++x) o[nt][x] *= f;
+    }
+  }
+  // The results of column nt, block row `br`, (token, head) row `row`; l is the whole sum.
+  __device__ __forceinline__ void write(int nt, const PagedTarget& to, const PagedAttendArgs& a, int64_t row, int br, int c) const {
+    if (to.final_rows) {
+      const float inv = l[nt] > 0.f ? 1.f / l[nt] : 0.f;
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int x = 0; x < NX; ++x)
+            store_elem(static_cast<T*>(a.out), row * D + d_first(p, c) + r * NX + x, o[nt][p * NX + x][r] * inv);
+      if (c == 0) a.lse[row] = l[nt] > 0.f ? (m[nt] + fast_log2(l[nt])) * kLn2 : -INFINITY;
+      return;
+    }
+    const int64_t at = to.by_row ? row : br;
+    if (c == 0) to.ml[at] = float2{m[nt], l[nt]};
+    if (l[nt] == 0.f) return;
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int x = 0; x < NX; x += 4)
+          *reinterpret_cast<f32x4*>(to.o + at * D + d_first(p, c) + r * NX + x) =
+              f32x4{o[nt][p * NX + x][r], o[nt][p * NX + x + 1][r], o[nt][p * NX + x + 2][r], o[nt][p * NX + x + 3][r]};
+  }
 
   __device__ __forceinline__ void load_k(const T* k, uint32_t rid, int i, int c, u32x4 (&kf)[2][NK]) const {
 #pragma unroll
@@ -292,166 +509,152 @@ struct PagedWave {
   }
 };
 
-template <typename T, int D, int NT>
-__global__ __launch_bounds__(256) void paged_stream_kernel(PagedAttendArgs a) {
-  using W = PagedWave<T, D, NT>;
-  constexpr int TK = 32, kWaves = 4;
-  // workgroups go to the XCDs in turn and the late splits of short caches are empty: the splits are rotated from head to head
-  const int rb = blockIdx.x / a.NS, g = blockIdx.y, b = blockIdx.z;
-  const int split = static_cast<int>((blockIdx.x - rb * a.NS + g + gridDim.y * b) % a.NS);
+constexpr int kStreamRows = 16, kStreamTile = 32;
+
+template <typename T, int D, bool kShare>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void paged_stream_kernel(PagedAttendArgs a) {
+  using W = PagedWave<T, D, 1>;
+  constexpr int TK = kStreamTile, kWaves = 4;
+  __shared__ f32x4 so[2][W::NACC][64];
+  __shared__ float sm[2][64], sl[2][64];
+  __shared__ uint32_t scratch[8];
   const int lane = threadIdx.x & 63, i = lane & 15, c = lane >> 4, wave = wave_index();
-  int64_t q0;
-  const int nq = query_range(a, b, q0), R = nq * a.G, r0 = rb * 16 * NT;
-  if (r0 >= R) return;
-  const int len = cache_rows(a, b);
-  const int past = len - nq;
-  const int pos_min = a.all_see_all ? len - 1 : past + r0 / a.G;
-  const int pos_max = a.all_see_all ? len - 1 : past + (min(r0 + 16 * NT, R) - 1) / a.G;
-  const KeyTiles<TK> kt(len, pos_min, pos_max, a.window, a.sinks);
-  const int u_end = min(kt.n, (split + 1) * a.tiles_per_split);
-  const int32_t* table = a.pages.table + b * a.pages.table_stride;
   const T* K = static_cast<const T*>(a.k);
   const T* V = static_cast<const T*>(a.v);
-
-  W w;
-  int64_t row[NT];                                         // (token, head) of this lane's column, -1: none
-  int pos[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = r0 + 16 * nt + i;
-    const bool valid = r < R;
+  PagedShare s = paged_share<kStreamRows, TK, kShare>(a, scratch);
+  const int g = s.g;
+  paged_blocks<kStreamRows, TK, kShare>(a, s, [&](const PagedBlock<kStreamRows, TK>& blk, int u0, int u1, bool begins) {
+    const int32_t* table = a.pages.table + blk.b * a.pages.table_stride;
+    const int r = blk.r0 + i;
+    const bool valid = r < blk.R;
     const int t = valid ? r / a.G : 0;
-    row[nt] = valid ? (q0 + t) * a.Hq + g * a.G + (r - t * a.G) : -1;
-    pos[nt] = !valid ? -1 : a.all_see_all ? len - 1 : past + t;
-    const T* qp = static_cast<const T*>(a.q) + (valid ? row[nt] : 0) * D + c * W::EPL;
-#pragma unroll
-    for (int kk = 0; kk < W::NK; ++kk) w.qf[nt][kk] = valid ? ld16(qp + kk * W::KD) : zero16();
-#pragma unroll
-    for (int x = 0; x < W::NACC; ++x) w.o[nt][x] = f32x4{0.f, 0.f, 0.f, 0.f};
-    w.m[nt] = -INFINITY;
-    w.l[nt] = 0.f;
-  }
-  auto row_of = [&](int u) -> uint32_t {                   // of row lane % 32 of the tile
-    int base, from, to;
-    kt.tile(u, base, from, to);
-    return page_row(a.pages, table, g, min(max(base + (lane & 31), from), to - 1));
-  };
-  int u = split * a.tiles_per_split + wave;
-  uint32_t rid = u < u_end ? row_of(u) : 0;
-  while (u < u_end) {
-    u32x4 kf[2][W::NK];
-    typename W::VPiece vf[8][W::NP];
-    w.load_k(K, rid, i, c, kf);
-    w.load_v(V, rid, i, c, vf);
-    int base, from, to;
-    kt.tile(u, base, from, to);
-    u += kWaves;
-    if (u < u_end) rid = row_of(u);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+    const int64_t row = (blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);     // where valid
+    const int pos = valid ? blk.pos_of(a, r) : -1;
+    W w;
+    w.clear();
+    w.load_q(0, static_cast<const T*>(a.q) + (valid ? row : 0) * D, valid, c);
+    auto row_of = [&](int u) -> uint32_t {                   // of row lane % 32 of the tile
+      int base, from, to;
+      blk.kt.tile(u, base, from, to);
+      return page_row(a.pages, table, g, min(max(base + (lane & 31), from), to - 1));
+    };
+    const int u_end = min(u1, blk.kt.n);
+    int u = u0 + wave;
+    uint32_t rid = u < u_end ? row_of(u) : 0;
+    while (u < u_end) {
+      u32x4 kf[2][W::NK];
+      typename W::VPiece vf[8][W::NP];
+      w.load_k(K, rid, i, c, kf);
+      w.load_v(V, rid, i, c, vf);
+      int base, from, to;
+      blk.kt.tile(u, base, from, to);
+      u += kWaves;
+      if (u < u_end) rid = row_of(u);
+      f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
       for (int kk = 0; kk < W::NK; ++kk)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) mma_step<T>(s[t], kf[t][kk], w.qf[nt][kk]);
-      float top = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int j = base + W::p_row(t, c, r);
-          const bool see = j >= from && j < to && j <= pos[nt] && (a.window == 0 || j > pos[nt] - a.window || j < a.sinks);
-          s[t][r] = see ? s[t][r] * a.sl2 : -INFINITY;
-          top = fmaxf(top, s[t][r]);
-        }
-      const float mn = fmaxf(w.m[nt], col4_max(top));
-      const float ref = mn == -INFINITY ? 0.f : mn;
-      const float f = mn == w.m[nt] ? 1.f : fast_exp2(w.m[nt] - ref);
-      w.m[nt] = mn;
-      float sum = 0.f;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) { s[t][r] = fast_exp2(s[t][r] - ref); sum += s[t][r]; }
-      w.l[nt] = w.l[nt] * f + sum;
-      if (__any(f != 1.f)) {
-#pragma unroll
-        for (int x = 0; x < W::NACC; ++x) w.o[nt][x] *= f;
-      }
+        for (int t2 = 0; t2 < 2; ++t2) mma_step<T>(sc[t2], kf[t2][kk], w.qf[0][kk]);
+      w.template weigh<2>(0, sc, 0, base, from, to, pos, a, c);
       // The weights are rounded to the type of V, the precision the matrix cores take them in.
       if constexpr (W::kBf16) {
-        const u32x4 pf = {pack_bf16x2(s[0][0], s[0][1]), pack_bf16x2(s[0][2], s[0][3]), pack_bf16x2(s[1][0], s[1][1]), pack_bf16x2(s[1][2], s[1][3])};
+        const u32x4 pf = {pack_bf16x2(sc[0][0], sc[0][1]), pack_bf16x2(sc[0][2], sc[0][3]), pack_bf16x2(sc[1][0], sc[1][1]), pack_bf16x2(sc[1][2], sc[1][3])};
 #pragma unroll
-        for (int x = 0; x < W::NX; ++x) mma_step<T>(w.o[nt][x], w.v_operand(vf, 0, x, 0), pf);
+        for (int x = 0; x < W::NX; ++x) mma_step<T>(w.o[0][x], w.v_operand(vf, 0, x, 0), pf);
       } else {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const u32x4 pf = __builtin_bit_cast(u32x4, s[t]);
+        for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
           for (int p = 0; p < W::NP; ++p)
 #pragma unroll
-            for (int x = 0; x < W::NX; ++x) mma_step<T>(w.o[nt][p * W::NX + x], w.v_operand(vf, p, x, t), pf);
-        }
+            for (int x = 0; x < W::NX; ++x) mma_step<T>(w.o[0][p * W::NX + x], w.v_operand(vf, p, x, t2), __builtin_bit_cast(u32x4, sc[t2]));
       }
     }
-  }
+    // The four waves' shares, joined pairwise through LDS: (2, 3) into (0, 1), then 1 into 0.
+    w.l[0] = col4_sum(w.l[0]);
+#pragma unroll
+    for (int half = 2; half >= 1; half >>= 1) {
+      if (wave >= half && wave < 2 * half) {
+#pragma unroll
+        for (int x = 0; x < W::NACC; ++x) so[wave - half][x][lane] = w.o[0][x];
+        sm[wave - half][lane] = w.m[0];
+        sl[wave - half][lane] = w.l[0];
+      }
+      __syncthreads();
+      if (wave < half) {
+        const float m2 = sm[wave][lane], mn = fmaxf(w.m[0], m2), ref = mn == -INFINITY ? 0.f : mn;
+        const float f = fast_exp2(w.m[0] - ref), f2 = fast_exp2(m2 - ref);
+        w.m[0] = mn;
+        w.l[0] = w.l[0] * f + sl[wave][lane] * f2;
+#pragma unroll
+        for (int x = 0; x < W::NACC; ++x) w.o[0][x] = w.o[0][x] * f + so[wave][x][lane] * f2;
+      }
+      __syncthreads();
+    }
+    const PagedTarget to = paged_target<kStreamRows, D, kShare>(a, s, blk, u0, u1, begins);
+    if (wave == 0 && valid) w.write(0, to, a, row, i, c);
+  });
+}
 
-  // The four waves' shares, joined pairwise through LDS: (2, 3) into (0, 1), then 1 into 0.
-  __shared__ f32x4 so[2][NT][W::NACC][64];
-  __shared__ float sm[2][NT][64], sl[2][NT][64];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) w.l[nt] = col4_sum(w.l[nt]);
-#pragma unroll
-  for (int half = 2; half >= 1; half >>= 1) {
-    if (wave >= half && wave < 2 * half) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-        for (int x = 0; x < W::NACC; ++x) so[wave - half][nt][x][lane] = w.o[nt][x];
-        sm[wave - half][nt][lane] = w.m[nt];
-        sl[wave - half][nt][lane] = w.l[nt];
-      }
-    }
-    __syncthreads();
-    if (wave < half) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float m2 = sm[wave][nt][lane], mn = fmaxf(w.m[nt], m2), ref = mn == -INFINITY ? 0.f : mn;
-        const float f = fast_exp2(w.m[nt] - ref), f2 = fast_exp2(m2 - ref);
-        w.m[nt] = mn;
-        w.l[nt] = w.l[nt] * f + sl[wave][nt][lane] * f2;
-#pragma unroll
-        for (int x = 0; x < W::NACC; ++x) w.o[nt][x] = w.o[nt][x] * f + so[wave][nt][x][lane] * f2;
-      }
-    }
-    __syncthreads();
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(8))) short s16x8;
+
+// The stream of tiles into LDS, 16 bytes a lane and load: wave w of 4 brings rows w, w + 1, .. of a quarter of a tile.  kSwzV: which
+// rows' pieces of V are permuted (see the kernels).
+template <typename T, int D>
+struct PagedTiles {
+  static constexpr bool kBf16 = sizeof(T) == 2;
+  static constexpr int TK = kBf16 ? 64 : 32, kRows = kBf16 ? 128 : 64;
+  static constexpr int kRowBytes = D * static_cast<int>(sizeof(T)), kChunks = kRowBytes / 16;
+  static constexpr int kPerLoad = 64 / kChunks, kWaveRows = TK / 4, kLoads = kWaveRows / kPerLoad;      // rows of a load, of a wave
+  static constexpr int kBytes = TK * kRowBytes;
+
+  const PagedAttendArgs& a;
+  const int32_t* table;
+  int g, wave, lane;
+  int entry, at_row;                                   // lane % kWaveRows: the page of one of the wave's rows of the tile looked up last
+
+  __device__ __forceinline__ void look_up(const KeyTiles<TK>& kt, int u) {
+    int base, from, to;
+    kt.tile(u, base, from, to);
+    const int p = min(max(base + kWaveRows * wave + lane % kWaveRows, from), to - 1);
+    const int e = page_div(p, a.pages.div);
+    at_row = p - e * a.pages.page_size;
+    entry = table[e];
   }
-  if (wave != 0) return;
+  __device__ __forceinline__ uint32_t row_number() const {
+    const int page = min(max(entry, 0), a.pages.n_pages - 1);
+    return (static_cast<uint32_t>(page) * a.pages.Hkv + g) * a.pages.page_size + at_row;
+  }
+  // LDS serves 16 lanes of 16 bytes (32 of 8) at a time, from 64 banks: 256 bytes.  K: those lanes have 16 rows in a row; V: 4.
+  static __device__ __forceinline__ int swizzle_k(int r) { return kRowBytes == 128 ? (r >> 1) & 7 : r & 15; }
+  static __device__ __forceinline__ int swizzle_v(int r) { return !kBf16 ? 0 : D == 128 ? 4 * (r & 3) : 2 * (r & 2); }
+  // the wave's rows of K or V of a tile on their way to `dst`; swizzle(row % 8): XORed to the index of a 16-byte piece
+  template <typename S>
+  __device__ __forceinline__ void issue(const void* src, uint32_t rid, char* dst, S&& swizzle) const {
+    const int sub = lane / kChunks, piece = lane % kChunks;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    if (row[nt] < 0) continue;
-    if (a.slots > 1) {
-      const int64_t at = row[nt] * a.slots + a.slot0 + split;
-      if (c == 0) a.part_ml[at] = float2{w.m[nt], w.l[nt]};
-      if (w.l[nt] == 0.f) continue;
-#pragma unroll
-      for (int p = 0; p < W::NP; ++p)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int x = 0; x < W::NX; ++x) a.part_o[at * D + W::d_first(p, c) + r * W::NX + x] = w.o[nt][p * W::NX + x][r];
-    } else {
-      const float inv = w.l[nt] > 0.f ? 1.f / w.l[nt] : 0.f;
-#pragma unroll
-      for (int p = 0; p < W::NP; ++p)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-          for (int x = 0; x < W::NX; ++x)
-            store_elem(static_cast<T*>(a.out), row[nt] * D + W::d_first(p, c) + r * W::NX + x, w.o[nt][p * W::NX + x][r] * inv);
-      if (c == 0) a.lse[row[nt]] = w.l[nt] > 0.f ? (w.m[nt] + fast_log2(w.l[nt])) * kLn2 : -INFINITY;
+    for (int n = 0; n < kLoads; ++n) {
+      const int r = n * kPerLoad + sub;                // of the wave's rows, whose number is a multiple of 8
+      const int64_t off = static_cast<int64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(rid), r))) * kRowBytes;
+      load_to_lds16(static_cast<const char*>(src) + off + (piece ^ swizzle(r)) * 16, dst + (kWaveRows * wave + n * kPerLoad) * kRowBytes);
     }
   }
+  __device__ __forceinline__ void issue_k(uint32_t rid, char* dst) const {
+    issue(a.k, rid, dst, [this](int r) { return swizzle_k(kWaveRows * wave + r); });
+  }
+  __device__ __forceinline__ void issue_v(uint32_t rid, char* dst) const {
+    issue(a.v, rid, dst, [](int r) { return swizzle_v(r); });
+  }
+  __device__ __forceinline__ void landed() {
+    stage_barrier();
+    asm volatile("" : "+v"(entry));                    // looked at behind the wait of the barrier only
+  }
+};
+
+__device__ __forceinline__ f32x16 mma32(const u32x4& a, const u32x4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
 // Many queries: the tiles of 64 rows go through LDS, where the 4 waves of a workgroup share them, 32 (token, head) rows of a
@@ -466,294 +669,362 @@ __global__ __launch_bounds__(256) void paged_stream_kernel(PagedAttendArgs a) {
 //
 // Sums are taken against a reference that follows the maximum only when a tile exceeds it by 2^8 (any reference gives the
 // same result while nothing overflows), so that the outputs are rarely rescaled.
-typedef __attribute__((ext_vector_type(16))) float f32x16;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-
-template <int D>
-struct PagedTile {
-  static constexpr int TK = 64, kRows = 128, kWaves = 4;
-  static constexpr int kRowBytes = 2 * D, kChunks = D / 8;         // 16-byte pieces of a row
-  static constexpr int kPerLoad = 64 / kChunks;                    // rows of one load instruction
-  static constexpr int kLoads = TK / kWaves / kPerLoad;
-  static constexpr int kTileBytes = TK * kRowBytes;
-  static constexpr int NS = D / 16, ND = D / 32;
-};
-
-__device__ __forceinline__ f32x16 mma32(const u32x4& a, const u32x4& b, const f32x16& c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-
-template <int D>
+template <int D, bool kShare>
 __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
-  using P = PagedTile<D>;
-  constexpr int TK = P::TK;
-  __shared__ __attribute__((aligned(16))) char s_k[2][P::kTileBytes], s_v[2][P::kTileBytes];
-  // workgroups of a (sequence, KV head) behind one L2, the heads of every sequence spread over the XCDs; the longest rows of a
-  // prompt first
-  int x = blockIdx.x, gb = blockIdx.y + gridDim.y * blockIdx.z;
-  if ((gridDim.y * gridDim.z) % 8 == 0) {
-    const int64_t at = x + static_cast<int64_t>(gridDim.x) * gb;
-    const int64_t slot = at / 8;
-    x = static_cast<int>(slot % gridDim.x);
-    gb = static_cast<int>(slot / gridDim.x) * 8 + static_cast<int>(at % 8);
-  }
-  const int g = gb % a.pages.Hkv, b = gb / a.pages.Hkv;
-  const int blocks = static_cast<int>(gridDim.x) / a.NS;
-  const int split = x % a.NS, rb = blocks - 1 - x / a.NS;
+  using P = PagedTiles<bf16_t, D>;
+  constexpr int TK = P::TK, kRows = P::kRows, NS = D / 16, ND = D / 32;
+  __shared__ __attribute__((aligned(16))) char s_k[2][P::kBytes], s_v[2][P::kBytes];
   const int lane = threadIdx.x & 63, wave = wave_index(), col = lane & 31, h = lane >> 5;
-  int64_t q0;
-  const int nq = query_range(a, b, q0), R = nq * a.G, r0 = rb * P::kRows;
-  if (r0 >= R) return;
-  const int len = cache_rows(a, b), past = len - nq;
-  const int pos_min = a.all_see_all ? len - 1 : past + r0 / a.G;
-  const int pos_max = a.all_see_all ? len - 1 : past + (min(r0 + P::kRows, R) - 1) / a.G;
-  const KeyTiles<TK> kt(len, pos_min, pos_max, a.window, a.sinks);
-  const int u0 = split * a.tiles_per_split, u_end = min(kt.n, u0 + a.tiles_per_split);
-
-  // this wave's rows
-  const int wr0 = r0 + 32 * wave, r = wr0 + col;
-  const bool valid = r < R, any_rows = wr0 < R;
-  const int t = valid ? r / a.G : 0;
-  const int64_t row = (q0 + t) * a.Hq + g * a.G + (r - t * a.G);       // where valid
-  const int pos = !valid ? -1 : a.all_see_all ? len - 1 : past + t;
-  const int wave_min = a.all_see_all ? len - 1 : past + wr0 / a.G;
-  const int wave_max = a.all_see_all ? len - 1 : past + (min(wr0 + 32, R) - 1) / a.G;
-  u32x4 qf[P::NS];
-#pragma unroll
-  for (int s = 0; s < P::NS; ++s)
-    qf[s] = valid ? ld16(static_cast<const uint16_t*>(a.q) + row * D + s * 16 + h * 8) : zero16();
-  f32x16 o[P::ND];
-#pragma unroll
-  for (int d = 0; d < P::ND; ++d)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
-  float ref = -INFINITY, l = 0.f;                      // reference (unscaled logits), this lane's share of the sum
-
-  // a tile's rows on their way: this wave brings 16 of them, lane % 16 looks up the page of one
-  const int32_t* table = a.pages.table + b * a.pages.table_stride;
-  int entry = 0, at_row = 0;
-  auto look_up = [&](int u) {
-    int base, from, to;
-    kt.tile(u, base, from, to);
-    const int p = min(max(base + 16 * wave + (lane & 15), from), to - 1);
-    const int e = page_div(p, a.pages.div);
-    at_row = p - e * a.pages.page_size;
-    entry = table[e];
-  };
-  auto row_number = [&]() -> uint32_t {
-    const int page = min(max(entry, 0), a.pages.n_pages - 1);
-    return (static_cast<uint32_t>(page) * a.pages.Hkv + g) * a.pages.page_size + at_row;
-  };
-  const int sub = lane / P::kChunks, piece = lane % P::kChunks;
-  auto issue = [&](uint32_t rid, char* kd, char* vd) {
-#pragma unroll
-    for (int n = 0; n < P::kLoads; ++n) {
-      const int in_wave = n * P::kPerLoad + sub;                     // row of the wave's 16
-      const int64_t off = static_cast<int64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(rid), in_wave))) * D;
-      load_to_lds16(static_cast<const uint16_t*>(a.k) + off + ((piece ^ (in_wave & 7)) * 8), kd + (16 * wave + n * P::kPerLoad) * P::kRowBytes);
-      load_to_lds16(static_cast<const uint16_t*>(a.v) + off + ((piece ^ (2 * (in_wave & 3))) * 8), vd + (16 * wave + n * P::kPerLoad) * P::kRowBytes);
-    }
-  };
-
+  PagedShare s = paged_share<kRows, TK, kShare>(a, reinterpret_cast<uint32_t*>(s_k[0]));
+  const int g = s.g;
   // offsets of this lane's reads
-  uint32_t k_off[4], v_off[2];
+  uint32_t k_off[NS], v_off[ND];
 #pragma unroll
-  for (int s = 0; s < 4; ++s) k_off[s] = col * P::kRowBytes + (((2 * s) ^ (h ^ (lane & 7))) * 16);
+  for (int st = 0; st < NS; ++st) k_off[st] = col * P::kRowBytes + (((2 * st + h) ^ P::swizzle_k(col)) * 16);
   const int li = lane & 15, dh = (lane >> 4) & 1;
 #pragma unroll
-  for (int d = 0; d < 2; ++d)
-    v_off[d] = (4 * h + (li >> 2)) * P::kRowBytes + (((4 * d) ^ (2 * dh + (li & 1)) ^ (2 * (li >> 2))) * 16) + ((li & 3) >> 1) * 8;
+  for (int d = 0; d < ND; ++d)
+    v_off[d] = (4 * h + (li >> 2)) * P::kRowBytes + (((4 * d + 2 * dh + (li & 1)) ^ P::swizzle_v(li >> 2)) * 16) + ((li & 3) >> 1) * 8;
 
-  auto step = [&](int u, const char* __restrict kc, const char* __restrict vc, char* __restrict kn, char* __restrict vn) __attribute__((always_inline)) {
-    const bool more = u + 1 < u_end;
-    if (more) {
-      const uint32_t rid = row_number();
-      if (u + 2 < u_end) look_up(u + 2);
-      issue(rid, kn, vn);
-    }
-    int base, from, to;
-    kt.tile(u, base, from, to);
-    if (any_rows && base <= wave_max) {
-      f32x16 s[2];
+  paged_blocks<kRows, TK, kShare>(a, s, [&](const PagedBlock<kRows, TK>& blk, int u0, int u1, bool begins) {
+    // this wave's rows
+    const int wr0 = blk.r0 + 32 * wave, r = wr0 + col;
+    const bool valid = r < blk.R, any_rows = wr0 < blk.R;
+    const int t = valid ? r / a.G : 0;
+    const int64_t row = (blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);       // where valid
+    const int pos = valid ? blk.pos_of(a, r) : -1;
+    const int wave_min = blk.pos_of(a, wr0), wave_max = blk.pos_of(a, min(wr0 + 32, blk.R) - 1);
+    u32x4 qf[NS];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+    for (int st = 0; st < NS; ++st) qf[st] = valid ? ld16(static_cast<const uint16_t*>(a.q) + row * D + st * 16 + h * 8) : zero16();
+    f32x16 o[ND];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[kb][e] = 0.f;
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int st = 0; st < P::NS; ++st) {
-          const u32x4 kf = *reinterpret_cast<const u32x4*>(kc + k_off[st & 3] + (st >> 2) * 128 + kb * 32 * P::kRowBytes);
-          s[kb] = mma32(kf, qf[st], s[kb]);
+      for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    float ref = -INFINITY, l = 0.f;                      // reference (unscaled logits), this lane's share of the sum
+    P tiles{a, a.pages.table + blk.b * a.pages.table_stride, g, wave, lane, 0, 0};
+    const int u_end = min(u1, blk.kt.n);
+    auto logits = [&](const char* __restrict kc, f32x16 (&sc)[2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[kb][e] = 0.f;
+#pragma unroll
+      for (int st = 0; st < NS; ++st)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const u32x4 kf = *reinterpret_cast<const u32x4*>(kc + k_off[st] + kb * 32 * P::kRowBytes);
+          sc[kb] = mma32(kf, qf[st], sc[kb]);
+        }
+    };
+    uint32_t rid = 0;                                    // this wave's rows of the tile that K was last requested of
+    // tile u, whose logits are sc: the next tile's logits are computed (from kc) among the exponentials of this one's
+    auto step = [&](int u, f32x16 (&sc)[2], f32x16 (&nx)[2], const char* __restrict kc, const char* __restrict vc, char* __restrict kn,
+                    char* __restrict vn) __attribute__((always_inline)) {
+      if (u + 1 < u_end) {
+        tiles.issue_v(rid, vn);
+        if (u + 2 < u_end) {
+          rid = tiles.row_number();
+          if (u + 3 < u_end) tiles.look_up(blk.kt, u + 3);
+          tiles.issue_k(rid, kn);
         }
       }
-      const bool full = base >= from && base + TK <= to && base + TK - 1 <= wave_min &&
-                        (a.window == 0 || base > wave_max - a.window || base + TK <= a.sinks);
-      if (!full) {
+      if (any_rows) {
+        int base, from, to;
+        blk.kt.tile(u, base, from, to);
+        const bool full = base >= from && base + TK <= to && base + TK - 1 <= wave_min &&
+                          (a.window == 0 || base > wave_max - a.window || base + TK <= a.sinks);
+        if (!full) {
+          // rows lo .. hi-1 of the cache, and where the range holds both, the first `sinks` rows
+          const int lo = a.window ? max(from, pos - a.window + 1) : from, hi = min(to, pos + 1);
+          const int first = base + 4 * h, sinks = a.window && base < a.sinks ? min(a.sinks, hi) : 0;
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int j = first + (32 * kb + 8 * (e >> 2) + (e & 3));
+              if (!((j >= lo && j < hi) || (j >= from && j < sinks))) sc[kb][e] = -INFINITY;
+            }
+        }
+        float top = sc[0][0];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int j = base + 32 * kb + 8 * (e >> 2) + 4 * h + (e & 3);
-            const bool see = j >= from && j < to && j <= pos && (a.window == 0 || j > pos - a.window || j < a.sinks);
-            if (!see) s[kb][e] = -INFINITY;
-          }
+          for (int e = 0; e < 16; ++e) top = fmaxf(top, sc[kb][e]);
+        float t0, t1;
+        pair32(top, t0, t1);
+        top = fmaxf(t0, t1);
+        if (__any((top - ref) * a.sl2 > 8.f)) {          // -inf - -inf is no number and asks for nothing
+          const float mn = fmaxf(ref, top), f = mn == ref ? 1.f : fast_exp2((ref - mn) * a.sl2);
+          ref = mn;
+          l *= f;
+#pragma unroll
+          for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[d][e] *= f;
+        }
+        const float shift = ref == -INFINITY ? 0.f : ref * a.sl2;
+        // the matrix products of this wave ahead of the other's exponentials
+        __builtin_amdgcn_s_setprio(1);
+        logits(kc, nx);
+        u32x4 pf[2][2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) { sc[kb][e] = fast_exp2(sc[kb][e] * a.sl2 - shift); l += sc[kb][e]; }
+          // rounded to bf16, what the matrix cores take
+#pragma unroll
+          for (int sh = 0; sh < 2; ++sh)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) pf[kb][sh][j] = pack_bf16x2(sc[kb][8 * sh + 2 * j], sc[kb][8 * sh + 2 * j + 1]);
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int sh = 0; sh < 2; ++sh)
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+              const char* vp = vc + v_off[d] + (32 * kb + 16 * sh) * P::kRowBytes;
+              typedef __attribute__((address_space(3))) s16x4* LdsPtr;
+              const s16x4 lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)vp);
+              const s16x4 hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(vp + 8 * P::kRowBytes));
+              const s16x8 vf = __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7);
+              o[d] = mma32(__builtin_bit_cast(u32x4, vf), pf[kb][sh], o[d]);
+            }
+        __builtin_amdgcn_s_setprio(0);
       }
-      float top = s[0][0];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, s[kb][e]);
-      float lo, hi;
-      pair32(top, lo, hi);
-      top = fmaxf(lo, hi);
-      if (__any((top - ref) * a.sl2 > 8.f)) {          // -inf - -inf is no number and asks for nothing
-        const float mn = fmaxf(ref, top), f = mn == ref ? 1.f : fast_exp2((ref - mn) * a.sl2);
-        ref = mn;
-        l *= f;
-#pragma unroll
-        for (int d = 0; d < P::ND; ++d)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[d][e] *= f;
+      tiles.landed();
+    };
+    if (u0 < u_end) {
+      f32x16 sa[2], sb[2];
+      tiles.look_up(blk.kt, u0);
+      rid = tiles.row_number();
+      if (u0 + 1 < u_end) tiles.look_up(blk.kt, u0 + 1);
+      tiles.issue_k(rid, s_k[0]);
+      tiles.issue_v(rid, s_v[0]);
+      if (u0 + 1 < u_end) {
+        rid = tiles.row_number();
+        if (u0 + 2 < u_end) tiles.look_up(blk.kt, u0 + 2);
+        tiles.issue_k(rid, s_k[1]);
       }
-      const float shift = ref == -INFINITY ? 0.f : ref * a.sl2;
-      u32x4 pf[2][2];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) { s[kb][e] = fast_exp2(s[kb][e] * a.sl2 - shift); l += s[kb][e]; }
-        // rounded to bf16, what the matrix cores take
-#pragma unroll
-        for (int sh = 0; sh < 2; ++sh)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) pf[kb][sh][j] = pack_bf16x2(s[kb][8 * sh + 2 * j], s[kb][8 * sh + 2 * j + 1]);
+      tiles.landed();
+      logits(s_k[0], sa);
+      tiles.landed();                                    // the first step overwrites what was read here
+      int u = u0;
+      for (; u + 1 < u_end; u += 2) {
+        step(u, sa, sb, s_k[1], s_v[0], s_k[0], s_v[1]);
+        step(u + 1, sb, sa, s_k[0], s_v[1], s_k[1], s_v[0]);
       }
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int sh = 0; sh < 2; ++sh)
-#pragma unroll
-          for (int d = 0; d < P::ND; ++d) {
-            const char* vp = vc + v_off[d & 1] + (d >> 1) * 128 + (32 * kb + 16 * sh) * P::kRowBytes;
-            typedef __attribute__((address_space(3))) s16x4* LdsPtr;
-            const s16x4 lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)vp);
-            const s16x4 hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(vp + 8 * P::kRowBytes));
-            typedef __attribute__((ext_vector_type(8))) short s16x8;
-            const s16x8 vf = __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7);
-            o[d] = mma32(__builtin_bit_cast(u32x4, vf), pf[kb][sh], o[d]);
-          }
+      if (u < u_end) step(u, sa, sb, s_k[1], s_v[0], s_k[0], s_v[1]);
     }
-    stage_barrier();
-    asm volatile("" : "+v"(entry));                    // looked at behind the wait of the barrier only
-  };
-  if (u0 < u_end) {
-    look_up(u0);
-    const uint32_t rid = row_number();
-    if (u0 + 1 < u_end) look_up(u0 + 1);
-    issue(rid, s_k[0], s_v[0]);
-    stage_barrier();
-    asm volatile("" : "+v"(entry));
-    int u = u0;
-    for (; u + 1 < u_end; u += 2) {
-      step(u, s_k[0], s_v[0], s_k[1], s_v[1]);
-      step(u + 1, s_k[1], s_v[1], s_k[0], s_v[0]);
+    const PagedTarget to = paged_target<kRows, D, kShare>(a, s, blk, u0, u1, begins);
+    float lo, hi;
+    pair32(l, lo, hi);
+    l = lo + hi;
+    const float m = ref * a.sl2;                           // log2 units
+    if (!valid) return;
+    if (to.final_rows) {
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      uint16_t* out = static_cast<uint16_t*>(a.out) + row * D;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; e += 8) {
+          u32x4 w;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(o[d][e + 2 * j] * inv, o[d][e + 2 * j + 1] * inv);
+          st16(out + 32 * d + 2 * e + 8 * h, w);
+        }
+      if (h == 0) a.lse[row] = l > 0.f ? (m + fast_log2(l)) * kLn2 : -INFINITY;
+      return;
     }
-    if (u < u_end) step(u, s_k[0], s_v[0], s_k[1], s_v[1]);
-  }
-  if (!valid) return;
-  float lo, hi;
-  pair32(l, lo, hi);
-  l = lo + hi;
-  const float m = ref * a.sl2;                           // log2 units
-  if (a.slots > 1) {
-    const int64_t at = row * a.slots + a.slot0 + split;
-    if (h == 0) a.part_ml[at] = float2{m, l};
+    const int64_t at = to.by_row ? row : r - blk.r0;
+    if (h == 0) to.ml[at] = float2{m, l};
     if (l == 0.f) return;
 #pragma unroll
-    for (int d = 0; d < P::ND; ++d)
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int e = 0; e < 16; e += 4)
-        *reinterpret_cast<f32x4*>(a.part_o + at * D + 32 * d + 16 * (e >> 3) + 8 * h + (e & 4)) = f32x4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
-  } else {
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    uint16_t* out = static_cast<uint16_t*>(a.out) + row * D;
-#pragma unroll
-    for (int d = 0; d < P::ND; ++d)
-#pragma unroll
-      for (int e = 0; e < 16; e += 8) {
-        u32x4 w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = pack_bf16x2(o[d][e + 2 * j] * inv, o[d][e + 2 * j + 1] * inv);
-        st16(out + 32 * d + 2 * e + 8 * h, w);
-      }
-    if (h == 0) a.lse[row] = l > 0.f ? (m + fast_log2(l)) * kLn2 : -INFINITY;
-  }
+        *reinterpret_cast<f32x4*>(to.o + at * D + 32 * d + 16 * (e >> 3) + 8 * h + (e & 4)) = f32x4{o[d][e], o[d][e + 1], o[d][e + 2], o[d][e + 3]};
+  });
 }
 
-// The partial results of a (token, head) joined, by W waves: 1 where a workgroup joins four rows, 4 where the rows are few and
-// their partials many.  A partial without any row has no output, only its (maximum, sum).  Tokens that no sequence owns are left
-// as they are.
-constexpr int kJoinSlots = 256;                            // most partials of a row
+// The same in fp32, tiles of 32 rows, products of 16 x 16 x 4: the layouts of the streaming kernel, with 16 rows to a wave and the
+// operands read from LDS 16 rows of the cache at a time.  Bound by the products.
+template <int D, bool kShare>
+__global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a) {
+  using P = PagedTiles<float, D>;
+  using W = PagedWave<float, D, 1>;
+  constexpr int TK = P::TK, kRows = P::kRows;
+  __shared__ __attribute__((aligned(16))) char s_k[2][P::kBytes], s_v[2][P::kBytes];
+  const int lane = threadIdx.x & 63, wave = wave_index(), i = lane & 15, c = lane >> 4;
+  PagedShare s = paged_share<kRows, TK, kShare>(a, reinterpret_cast<uint32_t*>(s_k[0]));
+  const int g = s.g;
+  paged_blocks<kRows, TK, kShare>(a, s, [&](const PagedBlock<kRows, TK>& blk, int u0, int u1, bool begins) {
+    const int wr0 = blk.r0 + 16 * wave, r = wr0 + i;
+    const bool any_rows = wr0 < blk.R;
+    const int wave_max = blk.pos_of(a, min(wr0 + 16, blk.R) - 1);
+    const bool valid = r < blk.R;
+    const int t0 = valid ? r / a.G : 0;
+    const int64_t row = (blk.q0 + t0) * a.Hq + g * a.G + (r - t0 * a.G);     // where valid
+    const int pos = valid ? blk.pos_of(a, r) : -1;
+    W w;
+    w.clear();
+    w.load_q(0, static_cast<const float*>(a.q) + (valid ? row : 0) * D, valid, c);
+    P tiles{a, a.pages.table + blk.b * a.pages.table_stride, g, wave, lane, 0, 0};
+    const int u_end = min(u1, blk.kt.n);
+    auto step = [&](int u, const char* __restrict kc, const char* __restrict vc, char* __restrict kn, char* __restrict vn) __attribute__((always_inline)) {
+      if (u + 1 < u_end) {
+        const uint32_t rid = tiles.row_number();
+        if (u + 2 < u_end) tiles.look_up(blk.kt, u + 2);
+        tiles.issue_k(rid, kn);
+        tiles.issue_v(rid, vn);
+      }
+      int base, from, to;
+      blk.kt.tile(u, base, from, to);
+      if (any_rows && base <= wave_max) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          f32x4 sc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int kk = 0; kk < W::NK; ++kk)
+            mma_step<float>(sc, *reinterpret_cast<const u32x4*>(kc + (16 * t + i) * P::kRowBytes + (((4 * kk + c) ^ P::swizzle_k(i)) * 16)), w.qf[0][kk]);
+          w.template weigh<1>(0, &sc, t, base, from, to, pos, a, c);
+#pragma unroll
+          for (int p = 0; p < W::NP; ++p) {
+            u32x4 vf[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) vf[y] = *reinterpret_cast<const u32x4*>(vc + (16 * t + 4 * c + y) * P::kRowBytes + p * 256 + i * 16);
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              mma_step<float>(w.o[0][p * 4 + x], u32x4{vf[0][x], vf[1][x], vf[2][x], vf[3][x]}, __builtin_bit_cast(u32x4, sc));
+          }
+        }
+      }
+      tiles.landed();
+    };
+    if (u0 < u_end) {
+      tiles.look_up(blk.kt, u0);
+      const uint32_t rid = tiles.row_number();
+      if (u0 + 1 < u_end) tiles.look_up(blk.kt, u0 + 1);
+      tiles.issue_k(rid, s_k[0]);
+      tiles.issue_v(rid, s_v[0]);
+      tiles.landed();
+      int u = u0;
+      for (; u + 1 < u_end; u += 2) {
+        step(u, s_k[0], s_v[0], s_k[1], s_v[1]);
+        step(u + 1, s_k[1], s_v[1], s_k[0], s_v[0]);
+      }
+      if (u < u_end) step(u, s_k[0], s_v[0], s_k[1], s_v[1]);
+    }
+    const PagedTarget to = paged_target<kRows, D, kShare>(a, s, blk, u0, u1, begins);
+    w.l[0] = col4_sum(w.l[0]);
+    if (valid) w.write(0, to, a, row, r - blk.r0, c);
+  });
+}
 
+// ---- joining the parts --------------------------------------------------------------------------------------------------
+
+struct PagedSide {             // the partials of one launch
+  int blocks, share, rows;     // as there; rows of a block
+  const int4* cut;
+  const float* part_o; const float2* part_ml;
+  const float* whole_o; const float2* whole_ml;
+};
+struct PagedJoinArgs {
+  PagedSide side[2];           // the sequences' own caches, a prefix (rows 0: none)
+  const int32_t* q_off;
+  int64_t total_q;
+  int Hq, G, Hkv, max_q_len;
+  void* out; float* lse;
+};
+
+// The partial results of a (token, head) joined, by W waves: 1 where a workgroup joins four rows, 4 where rows are few and their
+// parts many.  A part without any row of the cache has no output, only its (maximum, sum).
 template <typename T, int D, int W>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttendArgs a) {
-  constexpr int N = D / 64, NJ = kJoinSlots / 64, U = 4;
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedJoinArgs a) {
+  constexpr int N = D / 64, U = 4;
+  typedef float vec __attribute__((ext_vector_type(N)));
   const int lane = threadIdx.x & 63, wave = wave_index(), part = wave % W;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * (4 / W) + wave / W;
-  const int64_t q_first = a.q_off ? a.q_off[0] : 0, q_end = a.q_off ? min(static_cast<int64_t>(a.q_off[a.batch]), a.total_q) : a.total_q;
-  const int64_t token = row / a.Hq;
-  const bool owned = token >= q_first && token < q_end;
-  if (W == 1 && !owned) return;
-  const float2* ml = a.part_ml + (owned ? row : 0) * a.slots;
-  float2 x[NJ];
-  float top = -INFINITY;
+  const int g = blockIdx.y, b = blockIdx.z, r = static_cast<int>(blockIdx.x) * (4 / W) + wave / W;
+  int64_t q0 = b, q1 = b + 1;
+  if (a.q_off) { q0 = a.q_off[b]; q1 = a.q_off[b + 1]; }
+  q0 = min(max(q0, static_cast<int64_t>(0)), a.total_q);
+  q1 = min(max(q1, q0), a.total_q);
+  const int t = r / a.G;
+  if (t >= min(q1 - q0, static_cast<int64_t>(a.max_q_len))) return;
+  const int64_t row = (q0 + t) * a.Hq + g * a.G + (r - t * a.G);
+  // parts of each side: `first` .. and the rows of the block they are of
+  int n[2] = {0, 0}, w0[2] = {0, 0}, which[2] = {0, 0}, br[2] = {0, 0};
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    x[j] = 64 * j + lane < a.slots ? ml[64 * j + lane] : float2{-INFINITY, 0.f};
-    top = fmaxf(top, x[j].x);
+  for (int sd = 0; sd < 2; ++sd) {
+    const PagedSide& s = a.side[sd];
+    if (s.rows == 0) continue;
+    const int64_t at = sd == 0 ? r : q0 * a.G + r;
+    n[sd] = 1;
+    if (s.share == 0) { which[sd] = -1; continue; }
+    const int block = static_cast<int>(at / s.rows);
+    br[sd] = static_cast<int>(at - static_cast<int64_t>(block) * s.rows);
+    const int4 cut = s.cut[sd == 0 ? b * s.blocks + block : block];
+    w0[sd] = cut.x;
+    n[sd] = cut.y - cut.x + 1;
+    which[sd] = n[sd] == 1 ? -1 : cut.z;                   // -1: a whole block
   }
+  if (a.side[1].rows == 0 && which[0] < 0) return;         // already where it belongs
+  const int slots = n[0] + n[1];
+  float ref = -INFINITY, l = 0.f;
+  vec o = 0.f;
+  for (int base = 0; base < slots; base += 64) {
+    const int at = base + lane;
+    float2 ml{-INFINITY, 0.f};
+    const float* po = nullptr;
+    if (at < slots) {
+      const int sd = at >= n[0], k = at - (sd ? n[0] : 0);
+      const PagedSide& s = a.side[sd];
+      if (which[sd] < 0) {
+        ml = s.whole_ml[row];
+        po = s.whole_o + row * D;
+      } else {
+        const int64_t slot = ((static_cast<int64_t>(g) * s.share + w0[sd] + k) * 2 + (k == 0 ? which[sd] : 0)) * s.rows + br[sd];
+        ml = s.part_ml[slot];
+        po = s.part_o + slot * D;
+      }
+    }
+    float top = ml.x;
 #pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-  const float ref = top == -INFINITY ? 0.f : top;
-  float l = 0.f, f[NJ];
-#pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    f[j] = x[j].y > 0.f ? fast_exp2(x[j].x - ref) : 0.f;
-    l += x[j].y * f[j];
-  }
-  l = wave_sum(l);
-  float o[N] = {};
-  const float* po = a.part_o + (owned ? row : 0) * a.slots * D + lane * N;
-#pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    if (64 * j >= a.slots) break;
-    for (int s = part; s < min(64, a.slots - 64 * j); s += W * U) {
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    const float mn = fmaxf(ref, top), safe = mn == -INFINITY ? 0.f : mn;
+    const float back = fast_exp2(ref - safe);
+    const float f = ml.y > 0.f ? fast_exp2(ml.x - safe) : 0.f;
+    ref = mn;
+    l = l * back + wave_sum(ml.y * f);
+    o *= back;
+    const int here = min(64, slots - base);
+    const uint64_t p64 = reinterpret_cast<uint64_t>(po);
+    for (int k = part; k < here; k += W * U) {
       float w[U];
-      bool any = false;
+      vec v[U];
 #pragma unroll
       for (int y = 0; y < U; ++y) {
-        w[y] = s + W * y < 64 ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f[j]), min(s + W * y, 63))) : 0.f;
-        any |= w[y] != 0.f;
+        const int at2 = min(k + W * y, 63);
+        w[y] = k + W * y < here ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), at2)) : 0.f;
+        const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(p64), at2), hi = __builtin_amdgcn_readlane(static_cast<int>(p64 >> 32), at2);
+        const float* src = reinterpret_cast<const float*>((static_cast<uint64_t>(hi) << 32) | lo);
+        v[y] = 0.f;
+        if (w[y] != 0.f) v[y] = *reinterpret_cast<const vec*>(src + lane * N);
       }
-      if (!any) continue;
-      float v[U][N];
 #pragma unroll
-      for (int y = 0; y < U; ++y)
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[y][e] = w[y] != 0.f ? po[static_cast<int64_t>(64 * j + s + W * y) * D + e] : 0.f;
-#pragma unroll
-      for (int y = 0; y < U; ++y)
-#pragma unroll
-        for (int e = 0; e < N; ++e) o[e] += v[y][e] * w[y];
+      for (int y = 0; y < U; ++y) o += v[y] * w[y];
     }
   }
   if constexpr (W > 1) {
-    __shared__ float so[W][D];
-#pragma unroll
-    for (int e = 0; e < N; ++e) so[part][lane * N + e] = o[e];
+    __shared__ vec so[W][64];
+    so[part][lane] = o;
     __syncthreads();
-    if (part != 0 || !owned) return;
+    if (part != 0) return;
 #pragma unroll
-    for (int e = 0; e < N; ++e)
-      for (int w = 1; w < W; ++w) o[e] += so[w][lane * N + e];
+    for (int w = 1; w < W; ++w) o += so[w][lane];
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll

@@ -64,59 +64,101 @@ cd::Pages pages_of(const calidrop_paged_params* p, const int32_t* table, int64_t
   return pg;
 }
 
-// How an attention launch is cut up: rows (token, head of the group) of a workgroup, splits of the cache, tiles of a split.
-// Up to 32 rows stream the cache from memory to registers; more share tiles of it in LDS, in bf16 (fp32 products are sixteen
-// times slower than bf16 ones and wait for nothing).
-struct PagedPlan { int rows, NS, tiles; };
-constexpr int kPagedTile = 32;             // rows of a streamed tile, half those of a shared one
-constexpr int kPagedRowsAtOnce = 65536;    // rows of all workgroups, up to which a call is split further
-constexpr int kPagedMostSplits = 128;
-constexpr int kPagedMostRows = 128;
+// How an attention launch is cut up.  Up to 16 (token, head) rows stream the cache from memory to registers, more share tiles of
+// it in LDS.
+struct PagedPlan { bool stream; int rows, tile; int64_t blocks, items, share; };
+constexpr int kPagedStreamPlaces = 768, kPagedTilePlaces = 512;        // workgroups the chip holds at a time
+constexpr int kPagedLeastRows = 128;                                   // of the cache in a share
+constexpr int64_t kPagedMostItems = 4096;                              // every workgroup adds up their tiles
 
-// Rows of the longest cache that the queries of a call can see.
-int64_t paged_rows_seen(const calidrop_paged_params* p, int64_t max_q_len, int64_t max_len) {
-  if (!p->window) return max_len;
-  return std::min<int64_t>(max_len, static_cast<int64_t>(p->window) + p->sinks + max_q_len);
-}
-// Most tiles of `tile` rows that a workgroup of `rows` can need (cd::KeyTiles): under a window, the rows of the window and of the
-// sinks can begin and end inside a tile each, and share one.
+// Most tiles that a block can need (cd::KeyTiles): under a window, the rows of the window and of the sinks can begin and end
+// inside a tile each, and share one.
 int64_t most_tiles(const calidrop_paged_params* p, int64_t q_len, int64_t max_len, int64_t rows, int64_t tile) {
   const int64_t all = (max_len + tile - 1) / tile;
   if (!p->window) return all;
   const int64_t tokens = std::min(q_len, rows / (p->n_q_heads / p->n_kv_heads) + 2);
   return std::min(all + 1, (p->window + tokens + tile - 1) / tile + 1 + (p->sinks + tile - 1) / tile);
 }
-int most_paged_splits(int64_t seen) { return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kPagedMostSplits, (seen + 127) / 128))); }
 
-PagedPlan plan_paged(const calidrop_paged_params* p, int64_t sequences, int64_t q_len, int64_t total_q, int64_t max_len) {
-  const int64_t G = p->n_q_heads / p->n_kv_heads, rows = q_len * G;
-  PagedPlan plan;
-  plan.rows = rows <= 16 ? 16 : rows <= 32 || p->dtype == CALIDROP_FP32 ? 32 : kPagedMostRows;
-  const bool shared = plan.rows == kPagedMostRows;
-  const int64_t groups = p->n_kv_heads * std::max(sequences * ((rows + plan.rows - 1) / plan.rows), (total_q * G + plan.rows - 1) / plan.rows);
-  const int64_t most = shared ? kPagedRowsAtOnce / plan.rows : 2048;
-  const int64_t want = std::max<int64_t>(std::min<int64_t>(most_paged_splits(paged_rows_seen(p, q_len, max_len)), most / groups), 1);
-  const int64_t tile = shared ? 2 * kPagedTile : kPagedTile, unit = shared ? 2 : 4;     // no fewer than 128 rows
-  const int64_t tiles = most_tiles(p, q_len, max_len, plan.rows, tile);
-  plan.tiles = static_cast<int>(std::max((((tiles + want - 1) / want) + unit - 1) / unit * unit, unit));
-  plan.NS = static_cast<int>(std::max<int64_t>(1, (tiles + plan.tiles - 1) / plan.tiles));
+// Blocks, and the workgroups that could share a KV head.
+PagedPlan paged_blocks(const calidrop_paged_params* p, int64_t sequences, int64_t q_len, int64_t max_len) {
+  PagedPlan plan{};
+  const int64_t rows = q_len * (p->n_q_heads / p->n_kv_heads);
+  plan.stream = rows <= cd::kStreamRows;
+  const bool fp32 = p->dtype == CALIDROP_FP32;
+  plan.rows = plan.stream ? cd::kStreamRows : fp32 ? cd::PagedTiles<float, 128>::kRows : cd::PagedTiles<cd::bf16_t, 128>::kRows;
+  plan.tile = plan.stream || fp32 ? 32 : 64;
+  plan.blocks = (rows + plan.rows - 1) / plan.rows;
+  plan.items = sequences * plan.blocks;
+  const int64_t most = std::max<int64_t>(1, (plan.stream ? kPagedStreamPlaces : kPagedTilePlaces) / p->n_kv_heads);
+  const int64_t tiles = most_tiles(p, q_len, max_len, plan.rows, plan.tile);
+  plan.share = std::max<int64_t>(1, std::min(most, std::min(plan.items, kPagedMostItems) * tiles * plan.tile / kPagedLeastRows));
   return plan;
 }
 
-// Room for the partials of `rows` (token, head) rows: splits of a call make kPagedRowsAtOnce rows at most.
-size_t partial_rows(int64_t rows, int64_t seen) {
-  return static_cast<size_t>(std::min<int64_t>(rows * most_paged_splits(seen), kPagedRowsAtOnce));
+// A workgroup per block, or the tiles of a KV head shared evenly (and a launch that joins the parts): whichever is expected to take
+// less time, from the longest cache the host knows of.  Measured in 188 calls (1 to 64 sequences, 1 to 4096 queries, caches of 100
+// to 16512 rows, both types and head dimensions, 32 query and 8 KV heads), us a call, own block / shared:
+//   streams of one query, bf16, D = 128: 1 sequence of 300 rows 9.1 / 11.9, of 600 13.3 / 11.9, of 4000 78 / 14; 16 of 600 17.7 /
+//   20.1, of 1000 26.7 / 21.7, of 16000 364 / 174; 64 of 1000 46.6 / 55.3, of 4000 172 / 178.
+//   tiles, bf16, D = 128: 64 queries at 1000 rows 29 / 24, at 16000 359 / 44; 512 queries of a prompt 17.6 / 32.5, at 8512 rows
+//   193 / 102; 4 sequences of those 289 / 320; 2 prompts of 2048 87 / 170.
+// The host does not know how the lengths of several sequences differ.  The shared form does not care (4 chunks of 300 to 512
+// queries behind 8000 to 32000 rows 813 / 427, 64 queries of 1000 to 16000 rows 541 / 348), so it may cost `ragged` times the
+// other there.  Calls of many blocks level themselves out.
+struct PagedCost { float stream_tile, single, pair, pair_shared; };      // us a tile, alone on a compute unit and in pairs
+PagedPlan plan_paged(const calidrop_paged_params* p, int64_t sequences, int64_t q_len, int64_t max_len) {
+  constexpr PagedCost kCost[2][2] = {{{.4f, 1.05f, 1.33f, 1.4f}, {.6f, 1.35f, 2.1f, 2.25f}}, {{.7f, 1.9f, 2.7f, 2.7f}, {1.2f, 3.f, 5.f, 5.f}}};
+  const PagedCost& c = kCost[p->dtype == CALIDROP_FP32][p->head_dim == 128];
+  PagedPlan plan = paged_blocks(p, sequences, q_len, max_len);
+  const int64_t tiles = most_tiles(p, q_len, max_len, plan.rows, plan.tile), groups = plan.items * p->n_kv_heads;
+  if (plan.share == 1 || plan.items > kPagedMostItems || plan.items * tiles >= (int64_t{1} << 31) || groups >= 4 * kPagedTilePlaces) {
+    plan.share = 0;
+    return plan;
+  }
+  const float most = static_cast<float>(tiles), all = static_cast<float>(groups);
+  float own, shared, ragged;
+  if (plan.stream) {
+    const float traffic = all * most * 64.f * static_cast<float>(p->head_dim) * (p->dtype == CALIDROP_FP32 ? 4.f : 2.f) / 6.1e6f;
+    own = std::max(6.f + c.stream_tile * most, 3.f + traffic);
+    shared = 12.f + traffic;
+    ragged = 1.06f;
+  } else {
+    // the queries of a prompt see half of their own rows on average
+    const float mean = p->window ? most : std::max(most - .5f * static_cast<float>(q_len) / static_cast<float>(plan.tile), .5f * most);
+    const float places = kPagedTilePlaces, least = static_cast<float>(kPagedLeastRows / plan.tile);
+    const float parts = std::min(places, all * mean / least);
+    // as many blocks as places: the long ones end alone
+    own = 8.f + (groups <= kPagedTilePlaces / 2 ? c.single * most : groups <= kPagedTilePlaces ? c.pair * mean + c.single * (most - mean)
+                                                                                            : std::max(c.single * most, c.pair * mean * all / places));
+    shared = 14.f + 15.f * parts / places * static_cast<float>(plan.rows) / 128.f + c.pair_shared * std::max(mean * all / places, least);
+    ragged = groups <= 2 * kPagedTilePlaces ? 1.15f : 1.f;
+  }
+  if (shared >= own * (sequences > 1 ? ragged : 1.f)) plan.share = 0;
+  return plan;
 }
-size_t partial_bytes(const calidrop_paged_params* p, size_t rows) {
-  return round256(rows * sizeof(float2)) + round256(rows * p->head_dim * sizeof(float));
+
+// The workspace of a launch: how its blocks were cut, the parts, and with `keep` the whole blocks.
+struct PagedRegions { size_t cut, part_ml, part_o, whole_ml, whole_o, total; };
+PagedRegions paged_regions(const calidrop_paged_params* p, const PagedPlan& plan, int64_t total_q, bool keep) {
+  PagedRegions r{};
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t here = at; at += round256(bytes); return here; };
+  const size_t parts = static_cast<size_t>(plan.share) * p->n_kv_heads * 2 * plan.rows, whole = keep ? static_cast<size_t>(total_q) * p->n_q_heads : 0;
+  r.cut = take(static_cast<size_t>(std::min(plan.items, kPagedMostItems)) * sizeof(int4));
+  r.part_ml = take(parts * sizeof(float2));
+  r.part_o = take(parts * p->head_dim * sizeof(float));
+  r.whole_ml = take(whole * sizeof(float2));
+  r.whole_o = take(whole * p->head_dim * sizeof(float));
+  r.total = at;
+  return r;
 }
-size_t attend_bytes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len, int32_t max_cache_len) {
-  return std::max<size_t>(256, partial_bytes(p, partial_rows(total_q * p->n_q_heads, paged_rows_seen(p, max_q_len, max_cache_len))));
+size_t attend_bytes(const calidrop_paged_params* p, int64_t max_q_len, int64_t max_cache_len) {
+  return paged_regions(p, paged_blocks(p, p->batch, max_q_len, max_cache_len), 0, false).total;
 }
-size_t shared_bytes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len, int32_t max_cache_len, int32_t shared_len) {
-  const int64_t rows = total_q * p->n_q_heads;       // where a side is not split its partials are there all the same
-  return std::max<size_t>(256, partial_bytes(p, 2 * rows + partial_rows(rows, paged_rows_seen(p, max_q_len, max_cache_len)) +
-                                                    partial_rows(rows, shared_len)));
+size_t shared_bytes(const calidrop_paged_params* p, int64_t total_q, int64_t max_q_len, int64_t max_cache_len, int64_t shared_len) {
+  return paged_regions(p, paged_blocks(p, p->batch, max_q_len, max_cache_len), total_q, true).total +
+         paged_regions(p, paged_blocks(p, 1, total_q, shared_len), total_q, true).total;
 }
 
 int check_attend_sizes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len, int32_t max_cache_len) {
@@ -125,8 +167,10 @@ int check_attend_sizes(const calidrop_paged_params* p, int64_t total_q, int32_t 
                 static_cast<long long>(total_q), max_q_len, max_cache_len);
   if (total_q > (int64_t{1} << 30) / p->n_q_heads)
     return fail(CALIDROP_EUNSUPPORTED, "total_q * n_q_heads exceeds 2^30");
-  if (max_q_len > (int64_t{1} << 30) / p->n_q_heads)
-    return fail(CALIDROP_EUNSUPPORTED, "max_q_len * n_q_heads exceeds 2^30");
+  const int64_t G = p->n_q_heads / p->n_kv_heads;
+  if (max_q_len > (1 << 26) / G) return fail(CALIDROP_EUNSUPPORTED, "max_q_len * (n_q_heads / n_kv_heads) exceeds 2^26");
+  if ((max_q_len * G + 127) / 128 * p->n_kv_heads * p->batch >= 1 << 24)        // workgroups of 256 threads on one grid axis
+    return fail(CALIDROP_EUNSUPPORTED, "batch * max_q_len * n_q_heads exceeds 2^31");
   if (max_cache_len > paged_capacity(p))
     return fail(CALIDROP_ESHAPE, "max_cache_len %d exceeds the max_pages * page_size = %lld rows of a table", max_cache_len,
                 static_cast<long long>(paged_capacity(p)));
@@ -141,44 +185,48 @@ int check_shared_sizes(const calidrop_paged_params* p, int32_t shared_len) {
 }
 
 template <typename T, int D>
-int launch_paged(const cd::PagedAttendArgs& a, const PagedPlan& plan, int64_t sequences, int64_t q_len, hipStream_t st) {
-  const int64_t rows = q_len * a.G, blocks = (rows + plan.rows - 1) / plan.rows;
-  const dim3 grid(static_cast<unsigned>(blocks * plan.NS), a.pages.Hkv, static_cast<unsigned>(sequences));
-  if constexpr (sizeof(T) == 2) {
-    if (plan.rows == kPagedMostRows) {
-      hipLaunchKernelGGL((cd::paged_tile_kernel<D>), grid, dim3(256), 0, st, a);
-      return launch_status("paged_attend");
-    }
-  }
-  if (plan.rows == 16) hipLaunchKernelGGL((cd::paged_stream_kernel<T, D, 1>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((cd::paged_stream_kernel<T, D, 2>), grid, dim3(256), 0, st, a);
+int launch_paged(const calidrop_paged_params* p, cd::PagedAttendArgs a, const PagedPlan& plan, const PagedRegions& R, char* ws, bool keep,
+                 cd::PagedSide& side, hipStream_t st) {
+  a.blocks = static_cast<int>(plan.blocks); a.items = static_cast<int>(plan.items); a.share = static_cast<int>(plan.share);
+  a.least_tiles = kPagedLeastRows / plan.tile; a.keep = keep;
+  a.cut = reinterpret_cast<int4*>(ws + R.cut);
+  a.part_ml = reinterpret_cast<float2*>(ws + R.part_ml); a.part_o = reinterpret_cast<float*>(ws + R.part_o);
+  a.whole_ml = reinterpret_cast<float2*>(ws + R.whole_ml); a.whole_o = reinterpret_cast<float*>(ws + R.whole_o);
+  side.blocks = a.blocks; side.share = a.share; side.rows = plan.rows; side.cut = a.cut;
+  side.part_o = a.part_o; side.part_ml = a.part_ml; side.whole_o = a.whole_o; side.whole_ml = a.whole_ml;
+  const dim3 grid(static_cast<unsigned>((plan.share ? plan.share : plan.items) * p->n_kv_heads));
+  void (*kernel)(cd::PagedAttendArgs);
+  if (plan.stream) kernel = plan.share ? cd::paged_stream_kernel<T, D, true> : cd::paged_stream_kernel<T, D, false>;
+  else if constexpr (sizeof(T) == 2) kernel = plan.share ? cd::paged_tile_kernel<D, true> : cd::paged_tile_kernel<D, false>;
+  else kernel = plan.share ? cd::paged_tile32_kernel<D, true> : cd::paged_tile32_kernel<D, false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
   return launch_status("paged_attend");
 }
 
 // shared_table NULL: no prefix.
 template <typename T, int D>
-int attend_impl(const calidrop_paged_params* p, cd::PagedAttendArgs a, int32_t max_cache_len, const int32_t* shared_table,
-                int32_t shared_len, char* ws, hipStream_t st) {
-  const PagedPlan own = plan_paged(p, p->batch, a.max_q_len, a.total_q, max_cache_len);
-  PagedPlan prefix{};
-  if (shared_table) prefix = plan_paged(p, 1, a.total_q, a.total_q, shared_len);
-  a.slots = own.NS + prefix.NS;
-  a.part_ml = reinterpret_cast<float2*>(ws);
-  a.part_o = reinterpret_cast<float*>(ws + round256(static_cast<size_t>(a.total_q) * a.Hq * a.slots * sizeof(float2)));
+int attend_impl(const calidrop_paged_params* p, const cd::PagedAttendArgs& a, const int32_t* shared_table, int32_t shared_len, char* ws,
+                hipStream_t st) {
+  const bool keep = shared_table != nullptr;
+  const PagedPlan own = plan_paged(p, p->batch, a.max_q_len, a.max_len);
+  const PagedRegions own_r = paged_regions(p, own, a.total_q, keep);
+  cd::PagedJoinArgs j{};
   int rc;
   if (shared_table) {
+    const PagedPlan prefix = plan_paged(p, 1, a.total_q, shared_len);
     cd::PagedAttendArgs f = a;
     f.pages.table = shared_table; f.pages.table_stride = 0; f.lens = nullptr; f.fixed_len = shared_len; f.max_len = shared_len;
-    f.all_see_all = 1; f.slot0 = own.NS; f.NS = prefix.NS; f.tiles_per_split = prefix.tiles;
-    if ((rc = launch_paged<T, D>(f, prefix, 1, a.total_q, st))) return rc;
+    f.all_see_all = 1; f.batch = 1;
+    if ((rc = launch_paged<T, D>(p, f, prefix, paged_regions(p, prefix, a.total_q, true), ws + own_r.total, true, j.side[1], st))) return rc;
   }
-  a.NS = own.NS; a.tiles_per_split = own.tiles;
-  if ((rc = launch_paged<T, D>(a, own, p->batch, a.max_q_len, st))) return rc;
-  if (a.slots == 1) return CALIDROP_OK;
-  static_assert(2 * kPagedMostSplits <= cd::kJoinSlots, "the joining waves hold every partial of a row");
-  const int64_t rows = a.total_q * a.Hq;
-  if (a.slots <= 8) hipLaunchKernelGGL((cd::paged_join_kernel<T, D, 1>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((cd::paged_join_kernel<T, D, 4>), dim3(static_cast<unsigned>(rows)), dim3(256), 0, st, a);
+  if ((rc = launch_paged<T, D>(p, a, own, own_r, ws, keep, j.side[0], st))) return rc;
+  if (!keep && own.share == 0) return CALIDROP_OK;
+  j.q_off = a.q_off; j.total_q = a.total_q; j.Hq = a.Hq; j.G = a.G; j.Hkv = p->n_kv_heads; j.max_q_len = a.max_q_len; j.out = a.out; j.lse = a.lse;
+  const int64_t rows = static_cast<int64_t>(a.max_q_len) * a.G;
+  if (rows * p->n_kv_heads * p->batch >= 4096)
+    hipLaunchKernelGGL((cd::paged_join_kernel<T, D, 1>), dim3(static_cast<unsigned>((rows + 3) / 4), p->n_kv_heads, p->batch), dim3(256), 0, st, j);
+  else
+    hipLaunchKernelGGL((cd::paged_join_kernel<T, D, 4>), dim3(static_cast<unsigned>(rows), p->n_kv_heads, p->batch), dim3(256), 0, st, j);
   return launch_status("paged_join");
 }
 
@@ -208,7 +256,7 @@ int attend_entry(const calidrop_paged_params* p, const void* q, const int32_t* q
   a.out = out; a.lse = lse;
   hipStream_t st = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
-#define CD_DISPATCH(T, D) return attend_impl<T, D>(p, a, max_cache_len, shared_table, shared_len, ws, st)
+#define CD_DISPATCH(T, D) return attend_impl<T, D>(p, a, shared_table, shared_len, ws, st)
   if (p->dtype == CALIDROP_BF16) {
     if (p->head_dim == 128) CD_DISPATCH(cd::bf16_t, 128);
     CD_DISPATCH(cd::bf16_t, 64);
@@ -295,7 +343,7 @@ int calidrop_paged_append(const calidrop_paged_params* p, const void* q, int64_t
 
 size_t calidrop_paged_attend_workspace_bytes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len, int32_t max_cache_len) {
   if (check_paged(p) != CALIDROP_OK || check_attend_sizes(p, total_q, max_q_len, max_cache_len) != CALIDROP_OK) return 0;
-  return attend_bytes(p, total_q, max_q_len, max_cache_len);
+  return attend_bytes(p, max_q_len, max_cache_len);
 }
 
 int calidrop_paged_attend(const calidrop_paged_params* p, const void* q, const int32_t* q_offsets, int64_t total_q, int32_t max_q_len,
@@ -305,7 +353,7 @@ int calidrop_paged_attend(const calidrop_paged_params* p, const void* q, const i
   if ((rc = check_paged(p))) return rc;
   if ((rc = check_attend_sizes(p, total_q, max_q_len, max_cache_len))) return rc;
   return attend_entry(p, q, q_offsets, total_q, max_q_len, k_pages, v_pages, nullptr, 0, page_table, cache_lens, max_cache_len, out, lse,
-                      workspace, workspace_bytes, attend_bytes(p, total_q, max_q_len, max_cache_len), stream);
+                      workspace, workspace_bytes, attend_bytes(p, max_q_len, max_cache_len), stream);
 }
 
 size_t calidrop_paged_attend_shared_workspace_bytes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len,
