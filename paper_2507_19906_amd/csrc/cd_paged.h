@@ -14,8 +14,8 @@ namespace cd {
 
 // x / d for 0 <= x < 2^31 as one 64-bit product and shift: magic = ceil(2^shift / d), shift = 31 + ceil(log2 d).  magic < 2^32
 // and x * (magic * d - 2^shift) < 2^31 * d <= 2^shift, so the quotient is exact.
-struct PageDiv { uint32_t magic; int shift; };
-__device__ __forceinline__ int page_div(int x, PageDiv d) {
+struct Divisor { uint32_t magic; int shift; };
+__device__ __forceinline__ int divide(int x, Divisor d) {
   return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(x)) * d.magic) >> d.shift);
 }
 
@@ -23,13 +23,13 @@ struct Pages {
   const int32_t* table;      // entries of sequence b at table + b * table_stride
   int64_t table_stride;
   int page_size, n_pages, Hkv;
-  PageDiv div;
+  Divisor div;               // by page_size
 };
 
 // Row `pos` of KV head g as a row number of the page buffers (rows of D elements; below 2^32 for every buffer that fits the
 // card).  An entry that names no page is read as the nearest one that exists.
 __device__ __forceinline__ uint32_t page_row(const Pages& pg, const int32_t* table, int g, int pos) {
-  const int e = page_div(pos, pg.div);
+  const int e = divide(pos, pg.div);
   const int page = min(max(table[e], 0), pg.n_pages - 1);
   return (static_cast<uint32_t>(page) * pg.Hkv + g) * pg.page_size + (pos - e * pg.page_size);
 }
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
       }
       if (h >= Hq) {
         if (!fits) continue;
-        const int e = page_div(len + t, a.pages.div), page = table[e];
+        const int e = divide(len + t, a.pages.div), page = table[e];
         if (page < 0 || page >= a.pages.n_pages) continue;
         dst += ((static_cast<int64_t>(page) * Hkv + (h - Hq)) * a.pages.page_size + (len + t - e * a.pages.page_size)) * D * sizeof(T);
       }
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
       const int h = (r - turned) / kChunks;
       u = (r - turned) - h * kChunks;
       if (!fits) continue;
-      const int e = page_div(len + t, a.pages.div), page = table[e];
+      const int e = divide(len + t, a.pages.div), page = table[e];
       if (page < 0 || page >= a.pages.n_pages) continue;
       src = a.v + token * a.v_stride + static_cast<int64_t>(h) * D * sizeof(T);
       dst = a.v_pages + ((static_cast<int64_t>(page) * Hkv + h) * a.pages.page_size + (len + t - e * a.pages.page_size)) * D * sizeof(T);
@@ -183,45 +183,42 @@ __global__ __launch_bounds__(256) void paged_lens_kernel(PagedAppendArgs a) {
 // or, where there are too few blocks or their caches differ too much, a fixed number of workgroups shares the tiles of all
 // blocks of a KV head evenly, in order: a workgroup's share may begin and end inside a block.  The lengths are known to the
 // device alone, so each workgroup adds them up for itself.  Results of parts of blocks go to the workspace and are joined by a
-// second launch.
+// second launch.  A prefix that all sequences share is one more sequence, ahead of the others, whose queries are those of the
+// whole call and see every row; a (token, head) then has two blocks, whose results are joined.
 
 struct PagedAttendArgs {
   const void* q;             // [total_q][Hq][D]
   const int32_t* q_off;      // [batch+1], or NULL: one token each
   const void* k; const void* v;
-  const int32_t* lens;       // rows of each sequence's cache, or NULL: fixed_len rows
+  const int32_t* lens;       // rows of each sequence's cache
   Pages pages;
-  int fixed_len, max_len;
+  const int32_t* shared_table;
+  int shared_len, max_len;
   int64_t total_q;
   int batch, Hq, G, max_q_len;
+  Divisor by_G, by_blocks, by_Hkv;
   int window, sinks;         // window 0: no limit
-  int all_see_all;           // a prefix: every query sees every row
   float sl2;                 // scale * log2(e)
   void* out; float* lse;
-  int blocks, items;         // blocks of a sequence at most, of all sequences
+  int blocks, items;         // blocks of a sequence at most, of all sequences and the prefix
+  int prefix_items;          // those of the prefix come first; their results are kept apart
   int share;                 // workgroups that share the tiles of a KV head, 0: one per block
-  int least_tiles;           // of a share
-  int keep;                  // whole blocks go to the workspace too: they are joined with another launch's
+  int least_shift;           // a share has 2^least_shift tiles at least
   int4* cut;                 // [items] how a block was cut: first and last workgroup, 1 if it is not the first one's first
   float* part_o;             // [Hkv][share][2][kRows][D] the parts of the block a workgroup begins with, and of the one it ends with
   float2* part_ml;           // [Hkv][share][2][kRows]    unnormalised outputs; (maximum in log2 units, sum)
-  float* whole_o;            // keep: [total_q][Hq][D]
-  float2* whole_ml;          //       [total_q][Hq]
+  float* whole_o;            // with a prefix whole blocks go to the workspace too: [2][total_q][Hq][D], the prefix's second
+  float2* whole_ml;          // [2][total_q][Hq]
 };
 
 // The tokens of sequence b: first token and number.
 __device__ __forceinline__ int query_range(const PagedAttendArgs& a, int b, int64_t& q0) {
-  if (a.all_see_all) { q0 = 0; return static_cast<int>(a.total_q); }
   int64_t q1;
   if (a.q_off) { q0 = a.q_off[b]; q1 = a.q_off[b + 1]; } else { q0 = b; q1 = b + 1; }
   q0 = min(max(q0, static_cast<int64_t>(0)), a.total_q);
   q1 = min(max(q1, q0), a.total_q);
   return static_cast<int>(min(q1 - q0, static_cast<int64_t>(a.max_q_len)));
 }
-__device__ __forceinline__ int cache_rows(const PagedAttendArgs& a, int b) {
-  return a.lens ? min(max(a.lens[b], 0), a.max_len) : a.fixed_len;
-}
-
 // The tiles of TK rows that a block of queries needs: those that hold one of the first `sinks` rows, then those from the
 // oldest query's window to the newest query.  A tile takes part with the rows of its range only, so that a tile of both
 // ranges counts no row twice, and rows outside (freed pages, rows behind the end) are never read.
@@ -245,46 +242,65 @@ struct KeyTiles {
   }
 };
 
+// kSetup: tiles in whose time a workgroup gets ready for a block and hands over its results.  They count as tiles ahead of its own,
+// which a block's first workgroup has.
 template <int kRows, int TK>
 struct PagedBlock {
-  int b, nq, R, r0, len, past;
+  static constexpr int kSetup = kRows == 16 ? 4 : 3;
+  int R, r0, len, past;      // past: row of the first query, len in a prefix
+  bool prefix;
   int64_t q0;
+  const int32_t* table;
   KeyTiles<TK> kt;
   __device__ __forceinline__ void init(const PagedAttendArgs& a, int item) {
-    b = a.blocks == 1 ? item : item / a.blocks;
-    r0 = (item - b * a.blocks) * kRows;
-    nq = query_range(a, b, q0);
-    R = nq * a.G;
-    len = cache_rows(a, b);
-    past = len - nq;
+    prefix = item < a.prefix_items;
+    if (prefix) {
+      r0 = item * kRows;
+      q0 = 0;
+      R = static_cast<int>(a.total_q) * a.G;
+      past = len = a.shared_len;
+      table = a.shared_table;
+    } else {
+      item -= a.prefix_items;
+      const int b = divide(item, a.by_blocks);
+      r0 = (item - b * a.blocks) * kRows;
+      const int nq = query_range(a, b, q0);
+      R = nq * a.G;
+      len = min(max(a.lens[b], 0), a.max_len);
+      past = len - nq;
+      table = a.pages.table + b * a.pages.table_stride;
+    }
     kt.init(len, pos_of(a, r0), pos_of(a, min(r0 + kRows, R) - 1), a.window, a.sinks);
   }
   // the last row that block row r sees
-  __device__ __forceinline__ int pos_of(const PagedAttendArgs& a, int r) const { return a.all_see_all ? len - 1 : past + r / a.G; }
-  // tiles, 1 for a block whose queries see nothing, 0 where there is no such block
-  __device__ __forceinline__ uint32_t weight() const { return r0 < R ? max(kt.n, 1) : 0; }
+  __device__ __forceinline__ int pos_of(const PagedAttendArgs& a, int r) const { return past + divide(r, a.by_G); }
+  // tiles with those of the setup, 0 where there is no such block
+  __device__ __forceinline__ int weight() const { return r0 < R ? kt.n + kSetup : 0; }
 };
 
 // The tiles lo .. hi-1 of all blocks of KV head g are workgroup w's; they begin in block `item`, whose first tile is `start`.
-struct PagedShare { int lo, hi, start, total; int item, g, w, W; };      // tiles of a launch: below 2^31
+struct PagedShare { int lo, hi, start, total, each, more, item, g, w, W; };      // tiles of a launch: below 2^31
 
 template <int kRows, int TK, bool kShare>
 __device__ __forceinline__ PagedShare paged_share(const PagedAttendArgs& a, uint32_t* scratch) {
   PagedShare s;
   const int Hkv = a.pages.Hkv, x = blockIdx.x;
   PagedBlock<kRows, TK> blk;
-  s.lo = s.hi = s.start = s.w = s.W = 0;
+  s.lo = s.hi = s.start = s.w = s.W = s.each = s.more = 0;
   if constexpr (!kShare) {
     // blocks of a (sequence, KV head) behind one L2 and the heads of every sequence spread over the XCDs, which workgroups go
     // to in turn; the longest blocks of a prompt first
     const int heads = Hkv * a.batch;
     int rb, gb;
-    if (heads % 8 == 0) { const int slot = x / 8; rb = slot % a.blocks; gb = slot / a.blocks * 8 + x % 8; }
-    else { rb = x % a.blocks; gb = x / a.blocks; }
-    s.g = gb % Hkv;
-    s.item = gb / Hkv * a.blocks + (a.blocks - 1 - rb);
-    blk.init(a, s.item);
-    s.hi = s.total = blk.weight();
+    if (a.prefix_items) { gb = x % Hkv; rb = a.blocks - 1 - x / Hkv; }
+    else {
+      const int slot = heads % 8 == 0 ? x / 8 : x, gs = divide(slot, a.by_blocks);
+      rb = slot - gs * a.blocks;
+      gb = heads % 8 == 0 ? gs * 8 + x % 8 : gs;
+    }
+    const int b = divide(gb, a.by_Hkv);
+    s.g = gb - b * Hkv;
+    s.item = b * a.blocks + (a.blocks - 1 - rb);
     return s;
   }
   // the tiles of all blocks added up: a thread has up to (items + 255) / 256 blocks in a row
@@ -302,19 +318,21 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttendArgs& a, uint
     before = upto - mine + (tid >= 64 ? t0 : 0) + (tid >= 128 ? t1 : 0) + (tid >= 192 ? t2 : 0);
     s.total = __builtin_amdgcn_readfirstlane(t0 + t1 + t2 + t3);
   }
-  s.W = static_cast<int>(min(max(static_cast<uint32_t>(s.total) / a.least_tiles, 1u), static_cast<uint32_t>(a.share)));
+  s.W = min(max(s.total >> a.least_shift, 1), a.share);
   s.item = 0;
   if (s.W == a.share && 8 % Hkv == 0 && a.share % (8 / Hkv) == 0) {      // neighbouring shares behind one L2
     const int xcd = x % 8;
     s.g = xcd % Hkv;
     s.w = xcd / Hkv * (a.share / (8 / Hkv)) + x / 8;
   } else {
-    s.g = x % Hkv;
-    s.w = x / Hkv;
+    s.w = divide(x, a.by_Hkv);
+    s.g = x - s.w * Hkv;
   }
   if (s.w >= s.W) return s;
-  s.lo = static_cast<int64_t>(s.total) * s.w / s.W;
-  s.hi = static_cast<int64_t>(s.total) * (s.w + 1) / s.W;
+  s.each = static_cast<uint32_t>(s.total) / static_cast<uint32_t>(s.W);
+  s.more = s.total - s.each * s.W;                     // the first of them have one tile more
+  s.lo = s.each * s.w + min(s.w, s.more);
+  s.hi = s.lo + s.each + (s.w < s.more ? 1 : 0);
   if (a.items > 1) {
     if (before <= static_cast<uint32_t>(s.lo) && static_cast<uint32_t>(s.lo) < before + mine) {
       uint32_t at = before;
@@ -322,7 +340,7 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttendArgs& a, uint
       if (per > 1)
         for (; it < i1; ++it) {
           blk.init(a, it);
-          if (static_cast<uint32_t>(s.lo) < at + blk.weight()) break;
+          if (static_cast<uint32_t>(s.lo) < at + static_cast<uint32_t>(blk.weight())) break;
           at += blk.weight();
         }
       scratch[4] = it;
@@ -345,14 +363,16 @@ struct PagedTarget {
 template <int kRows, int D, bool kShare, int TK>
 __device__ __forceinline__ PagedTarget paged_target(const PagedAttendArgs& a, const PagedShare& s, const PagedBlock<kRows, TK>& blk, int u0, int u1,
                                                     bool begins) {
-  const int n = static_cast<int>(blk.weight());
-  if constexpr (!kShare) return PagedTarget{!a.keep, true, a.whole_o, a.whole_ml};
+  const int64_t side = blk.prefix ? a.total_q * a.Hq : 0;
+  const PagedTarget whole{a.prefix_items == 0, true, a.whole_o + side * D, a.whole_ml + side};
+  if constexpr (!kShare) return whole;
   if (s.g == 0 && u0 == 0 && threadIdx.x == 0) {
-    // the last workgroup whose share begins ahead of the block's end
-    const int last = static_cast<int>((static_cast<int64_t>(s.start + n) * s.W + s.total - 1) / s.total) - 1;
-    a.cut[s.item] = int4{s.w, last, begins ? 0 : 1, 0};
+    // the workgroup that the block's last tile is in the share of
+    const uint32_t x = s.start + blk.weight() - 1, longer = s.more * (s.each + 1);
+    const uint32_t last = x < longer ? x / (s.each + 1) : s.more + (x - longer) / s.each;
+    a.cut[s.item] = int4{s.w, static_cast<int>(last), begins ? 0 : 1, 0};
   }
-  if (u0 == 0 && u1 == n) return PagedTarget{!a.keep, true, a.whole_o, a.whole_ml};
+  if (u0 == 0 && u1 == blk.kt.n) return whole;
   const int64_t slot = (static_cast<int64_t>(s.g) * a.share + s.w) * 2 + (begins ? 0 : 1);
   return PagedTarget{false, false, a.part_o + slot * kRows * D, a.part_ml + slot * kRows};
 }
@@ -360,24 +380,26 @@ __device__ __forceinline__ PagedTarget paged_target(const PagedAttendArgs& a, co
 // f(block, u0, u1, first of the share) for every block that the workgroup has tiles u0 .. u1-1 of.
 template <int kRows, int TK, bool kShare, typename F>
 __device__ __forceinline__ void paged_blocks(const PagedAttendArgs& a, PagedShare& s, F&& f) {
+  PagedBlock<kRows, TK> blk;
   if constexpr (!kShare) {
-    PagedBlock<kRows, TK> blk;
     blk.init(a, s.item);
-    if (s.hi > 0) f(blk, 0, s.hi, true);
+    if (blk.r0 < blk.R) f(blk, 0, blk.kt.n, true);
     return;
   }
   bool begins = true;
   while (s.lo < s.hi) {
-    PagedBlock<kRows, TK> blk;
     blk.init(a, s.item);
-    const int n = static_cast<int>(blk.weight());
+    const int n = blk.weight();
     if (n > 0) {
-      const int u0 = s.lo - s.start, u1 = min(n, s.hi - s.start);
-      f(blk, u0, u1, begins);
-      begins = false;
-      s.lo = s.start + u1;
+      // a share that ends within the setup leaves the block to the next, one that begins there has it from its first tile on
+      const int u0 = max(s.lo - s.start - blk.kSetup, 0), u1 = min(n, s.hi - s.start) - blk.kSetup;
+      if (u1 > 0 || (u1 == 0 && blk.kt.n == 0)) {
+        f(blk, u0, u1, begins);
+        begins = false;
+      }
     }
     s.start += n;
+    s.lo = s.start;
     ++s.item;
   }
 }
@@ -524,10 +546,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void paged_stream_kern
   PagedShare s = paged_share<kStreamRows, TK, kShare>(a, scratch);
   const int g = s.g;
   paged_blocks<kStreamRows, TK, kShare>(a, s, [&](const PagedBlock<kStreamRows, TK>& blk, int u0, int u1, bool begins) {
-    const int32_t* table = a.pages.table + blk.b * a.pages.table_stride;
+    const int32_t* table = blk.table;
     const int r = blk.r0 + i;
     const bool valid = r < blk.R;
-    const int t = valid ? r / a.G : 0;
+    const int t = valid ? divide(r, a.by_G) : 0;
     const int64_t row = (blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);     // where valid
     const int pos = valid ? blk.pos_of(a, r) : -1;
     W w;
@@ -619,9 +641,23 @@ struct PagedTiles {
     int base, from, to;
     kt.tile(u, base, from, to);
     const int p = min(max(base + kWaveRows * wave + lane % kWaveRows, from), to - 1);
-    const int e = page_div(p, a.pages.div);
+    const int e = divide(p, a.pages.div);
     at_row = p - e * a.pages.page_size;
     entry = table[e];
+  }
+  // three at once: the rows of the first two, the third looked up
+  __device__ __forceinline__ void look_up(const KeyTiles<TK>& kt, int u, int u2, int u3, uint32_t& first, uint32_t& second) {
+    look_up(kt, u);
+    const int e1 = entry, r1 = at_row;
+    look_up(kt, u2);
+    const int e2 = entry, r2 = at_row;
+    look_up(kt, u3);
+    const int e3 = entry, r3 = at_row;
+    entry = e1; at_row = r1;
+    first = row_number();
+    entry = e2; at_row = r2;
+    second = row_number();
+    entry = e3; at_row = r3;
   }
   __device__ __forceinline__ uint32_t row_number() const {
     const int page = min(max(entry, 0), a.pages.n_pages - 1);
@@ -690,7 +726,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
     // this wave's rows
     const int wr0 = blk.r0 + 32 * wave, r = wr0 + col;
     const bool valid = r < blk.R, any_rows = wr0 < blk.R;
-    const int t = valid ? r / a.G : 0;
+    const int t = valid ? divide(r, a.by_G) : 0;
     const int64_t row = (blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);       // where valid
     const int pos = valid ? blk.pos_of(a, r) : -1;
     const int wave_min = blk.pos_of(a, wr0), wave_max = blk.pos_of(a, min(wr0 + 32, blk.R) - 1);
@@ -703,7 +739,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
     float ref = -INFINITY, l = 0.f;                      // reference (unscaled logits), this lane's share of the sum
-    P tiles{a, a.pages.table + blk.b * a.pages.table_stride, g, wave, lane, 0, 0};
+    P tiles{a, blk.table, g, wave, lane, 0, 0};
     const int u_end = min(u1, blk.kt.n);
     auto logits = [&](const char* __restrict kc, f32x16 (&sc)[2]) __attribute__((always_inline)) {
 #pragma unroll
@@ -798,16 +834,11 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
     };
     if (u0 < u_end) {
       f32x16 sa[2], sb[2];
-      tiles.look_up(blk.kt, u0);
-      rid = tiles.row_number();
-      if (u0 + 1 < u_end) tiles.look_up(blk.kt, u0 + 1);
-      tiles.issue_k(rid, s_k[0]);
-      tiles.issue_v(rid, s_v[0]);
-      if (u0 + 1 < u_end) {
-        rid = tiles.row_number();
-        if (u0 + 2 < u_end) tiles.look_up(blk.kt, u0 + 2);
-        tiles.issue_k(rid, s_k[1]);
-      }
+      uint32_t first = 0;
+      tiles.look_up(blk.kt, u0, min(u0 + 1, u_end - 1), min(u0 + 2, u_end - 1), first, rid);
+      tiles.issue_k(first, s_k[0]);
+      tiles.issue_v(first, s_v[0]);
+      if (u0 + 1 < u_end) tiles.issue_k(rid, s_k[1]);
       tiles.landed();
       logits(s_k[0], sa);
       tiles.landed();                                    // the first step overwrites what was read here
@@ -866,13 +897,13 @@ __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a)
     const bool any_rows = wr0 < blk.R;
     const int wave_max = blk.pos_of(a, min(wr0 + 16, blk.R) - 1);
     const bool valid = r < blk.R;
-    const int t0 = valid ? r / a.G : 0;
+    const int t0 = valid ? divide(r, a.by_G) : 0;
     const int64_t row = (blk.q0 + t0) * a.Hq + g * a.G + (r - t0 * a.G);     // where valid
     const int pos = valid ? blk.pos_of(a, r) : -1;
     W w;
     w.clear();
     w.load_q(0, static_cast<const float*>(a.q) + (valid ? row : 0) * D, valid, c);
-    P tiles{a, a.pages.table + blk.b * a.pages.table_stride, g, wave, lane, 0, 0};
+    P tiles{a, blk.table, g, wave, lane, 0, 0};
     const int u_end = min(u1, blk.kt.n);
     auto step = [&](int u, const char* __restrict kc, const char* __restrict vc, char* __restrict kn, char* __restrict vn) __attribute__((always_inline)) {
       if (u + 1 < u_end) {
@@ -905,9 +936,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a)
       tiles.landed();
     };
     if (u0 < u_end) {
-      tiles.look_up(blk.kt, u0);
-      const uint32_t rid = tiles.row_number();
-      if (u0 + 1 < u_end) tiles.look_up(blk.kt, u0 + 1);
+      uint32_t rid, none;
+      tiles.look_up(blk.kt, u0, u0, min(u0 + 1, u_end - 1), rid, none);
       tiles.issue_k(rid, s_k[0]);
       tiles.issue_v(rid, s_v[0]);
       tiles.landed();
@@ -926,52 +956,41 @@ __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a)
 
 // ---- joining the parts --------------------------------------------------------------------------------------------------
 
-struct PagedSide {             // the partials of one launch
-  int blocks, share, rows;     // as there; rows of a block
-  const int4* cut;
-  const float* part_o; const float2* part_ml;
-  const float* whole_o; const float2* whole_ml;
-};
 struct PagedJoinArgs {
-  PagedSide side[2];           // the sequences' own caches, a prefix (rows 0: none)
-  const int32_t* q_off;
-  int64_t total_q;
-  int Hq, G, Hkv, max_q_len;
-  void* out; float* lse;
+  PagedAttendArgs a;
+  int rows;                    // of a block
 };
 
-// The partial results of a (token, head) joined, by W waves: 1 where a workgroup joins four rows, 4 where rows are few and their
-// parts many.  A part without any row of the cache has no output, only its (maximum, sum).
+// The partial results of a (token, head) joined, by W waves: 1 where a workgroup joins four rows, more where rows are few and
+// their parts many.  A part without any row of the cache has no output, only its (maximum, sum).
 template <typename T, int D, int W>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedJoinArgs a) {
-  constexpr int N = D / 64, U = 4;
+__global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void paged_join_kernel(PagedJoinArgs j) {
+  constexpr int N = D / 64, U = 4, kRowsHere = W == 1 ? 4 : 1;
   typedef float vec __attribute__((ext_vector_type(N)));
+  const PagedAttendArgs& a = j.a;
   const int lane = threadIdx.x & 63, wave = wave_index(), part = wave % W;
-  const int g = blockIdx.y, b = blockIdx.z, r = static_cast<int>(blockIdx.x) * (4 / W) + wave / W;
-  int64_t q0 = b, q1 = b + 1;
-  if (a.q_off) { q0 = a.q_off[b]; q1 = a.q_off[b + 1]; }
-  q0 = min(max(q0, static_cast<int64_t>(0)), a.total_q);
-  q1 = min(max(q1, q0), a.total_q);
-  const int t = r / a.G;
-  if (t >= min(q1 - q0, static_cast<int64_t>(a.max_q_len))) return;
+  const int g = blockIdx.y, b = blockIdx.z, r = static_cast<int>(blockIdx.x) * kRowsHere + wave / W;
+  int64_t q0;
+  const int nq = query_range(a, b, q0), t = divide(r, a.by_G);
+  if (t >= nq) return;
   const int64_t row = (q0 + t) * a.Hq + g * a.G + (r - t * a.G);
-  // parts of each side: `first` .. and the rows of the block they are of
+  // parts of the own block and of the prefix's: first workgroup, number, rows of the block
   int n[2] = {0, 0}, w0[2] = {0, 0}, which[2] = {0, 0}, br[2] = {0, 0};
 #pragma unroll
   for (int sd = 0; sd < 2; ++sd) {
-    const PagedSide& s = a.side[sd];
-    if (s.rows == 0) continue;
+    if (sd == 1 && a.prefix_items == 0) continue;
     const int64_t at = sd == 0 ? r : q0 * a.G + r;
     n[sd] = 1;
-    if (s.share == 0) { which[sd] = -1; continue; }
-    const int block = static_cast<int>(at / s.rows);
-    br[sd] = static_cast<int>(at - static_cast<int64_t>(block) * s.rows);
-    const int4 cut = s.cut[sd == 0 ? b * s.blocks + block : block];
+    which[sd] = -1;                                        // a whole block
+    if (a.share == 0) continue;
+    const int block = static_cast<int>(at / j.rows);
+    br[sd] = static_cast<int>(at - static_cast<int64_t>(block) * j.rows);
+    const int4 cut = a.cut[sd == 0 ? a.prefix_items + b * a.blocks + block : block];
     w0[sd] = cut.x;
     n[sd] = cut.y - cut.x + 1;
-    which[sd] = n[sd] == 1 ? -1 : cut.z;                   // -1: a whole block
+    if (n[sd] > 1) which[sd] = cut.z;
   }
-  if (a.side[1].rows == 0 && which[0] < 0) return;         // already where it belongs
+  if (a.prefix_items == 0 && which[0] < 0) return;         // already where it belongs
   const int slots = n[0] + n[1];
   float ref = -INFINITY, l = 0.f;
   vec o = 0.f;
@@ -981,14 +1000,14 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedJoinArgs a) {
     const float* po = nullptr;
     if (at < slots) {
       const int sd = at >= n[0], k = at - (sd ? n[0] : 0);
-      const PagedSide& s = a.side[sd];
       if (which[sd] < 0) {
-        ml = s.whole_ml[row];
-        po = s.whole_o + row * D;
+        const int64_t at2 = row + (sd ? a.total_q * a.Hq : 0);
+        ml = a.whole_ml[at2];
+        po = a.whole_o + at2 * D;
       } else {
-        const int64_t slot = ((static_cast<int64_t>(g) * s.share + w0[sd] + k) * 2 + (k == 0 ? which[sd] : 0)) * s.rows + br[sd];
-        ml = s.part_ml[slot];
-        po = s.part_o + slot * D;
+        const int64_t slot = ((static_cast<int64_t>(g) * a.share + w0[sd] + k) * 2 + (k == 0 ? which[sd] : 0)) * j.rows + br[sd];
+        ml = a.part_ml[slot];
+        po = a.part_o + slot * D;
       }
     }
     float top = ml.x;

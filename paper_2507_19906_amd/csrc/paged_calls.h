@@ -49,8 +49,8 @@ int check_ptrs(const NamedPtr (&req)[N]) {
   return CALIDROP_OK;
 }
 
-// magic = ceil(2^shift / d) with shift = 31 + ceil(log2 d); see page_div
-cd::PageDiv page_divisor(int d) {
+// magic = ceil(2^shift / d) with shift = 31 + ceil(log2 d); see cd::divide
+cd::Divisor divisor(int d) {
   int bits = 0;
   while ((static_cast<int64_t>(1) << bits) < d) ++bits;
   const int shift = 31 + bits;
@@ -60,15 +60,14 @@ cd::PageDiv page_divisor(int d) {
 cd::Pages pages_of(const calidrop_paged_params* p, const int32_t* table, int64_t stride) {
   cd::Pages pg{};
   pg.table = table; pg.table_stride = stride; pg.page_size = p->page_size; pg.n_pages = p->n_pages; pg.Hkv = p->n_kv_heads;
-  pg.div = page_divisor(p->page_size);
+  pg.div = divisor(p->page_size);
   return pg;
 }
 
 // How an attention launch is cut up.  Up to 16 (token, head) rows stream the cache from memory to registers, more share tiles of
 // it in LDS.
-struct PagedPlan { bool stream; int rows, tile; int64_t blocks, items, share; };
+struct PagedPlan { bool stream; int rows, tile, least_shift; int64_t blocks, prefix, items, share, most_tiles; };      // share 0: a workgroup per block
 constexpr int kPagedStreamPlaces = 768, kPagedTilePlaces = 512;        // workgroups the chip holds at a time
-constexpr int kPagedLeastRows = 128;                                   // of the cache in a share
 constexpr int64_t kPagedMostItems = 4096;                              // every workgroup adds up their tiles
 
 // Most tiles that a block can need (cd::KeyTiles): under a window, the rows of the window and of the sinks can begin and end
@@ -80,19 +79,24 @@ int64_t most_tiles(const calidrop_paged_params* p, int64_t q_len, int64_t max_le
   return std::min(all + 1, (p->window + tokens + tile - 1) / tile + 1 + (p->sinks + tile - 1) / tile);
 }
 
-// Blocks, and the workgroups that could share a KV head.
-PagedPlan paged_blocks(const calidrop_paged_params* p, int64_t sequences, int64_t q_len, int64_t max_len) {
+// Blocks, and the workgroups that could share a KV head.  shared_len 0: no prefix.
+PagedPlan paged_blocks(const calidrop_paged_params* p, int64_t total_q, int64_t q_len, int64_t max_len, int64_t shared_len) {
   PagedPlan plan{};
-  const int64_t rows = q_len * (p->n_q_heads / p->n_kv_heads);
-  plan.stream = rows <= cd::kStreamRows;
+  const int64_t G = p->n_q_heads / p->n_kv_heads, rows = (shared_len ? std::max(total_q, q_len) : q_len) * G;
   const bool fp32 = p->dtype == CALIDROP_FP32;
+  plan.stream = rows <= cd::kStreamRows;
   plan.rows = plan.stream ? cd::kStreamRows : fp32 ? cd::PagedTiles<float, 128>::kRows : cd::PagedTiles<cd::bf16_t, 128>::kRows;
   plan.tile = plan.stream || fp32 ? 32 : 64;
-  plan.blocks = (rows + plan.rows - 1) / plan.rows;
-  plan.items = sequences * plan.blocks;
+  plan.least_shift = 2;                                 // tiles of a share at least, setup included
+  plan.blocks = (q_len * G + plan.rows - 1) / plan.rows;
+  plan.prefix = shared_len ? (total_q * G + plan.rows - 1) / plan.rows : 0;
+  plan.items = plan.prefix + p->batch * plan.blocks;
+  plan.most_tiles = most_tiles(p, q_len, max_len, plan.rows, plan.tile);
   const int64_t most = std::max<int64_t>(1, (plan.stream ? kPagedStreamPlaces : kPagedTilePlaces) / p->n_kv_heads);
-  const int64_t tiles = most_tiles(p, q_len, max_len, plan.rows, plan.tile);
-  plan.share = std::max<int64_t>(1, std::min(most, std::min(plan.items, kPagedMostItems) * tiles * plan.tile / kPagedLeastRows));
+  const int setup = plan.stream ? cd::PagedBlock<16, 32>::kSetup : cd::PagedBlock<128, 64>::kSetup;
+  const int64_t tiles = std::min(plan.prefix, kPagedMostItems) * ((shared_len + plan.tile - 1) / plan.tile + setup) +
+                        std::min(plan.items - plan.prefix, kPagedMostItems) * (plan.most_tiles + setup);
+  plan.share = std::max<int64_t>(1, std::min(most, tiles >> plan.least_shift));
   return plan;
 }
 
@@ -107,12 +111,17 @@ PagedPlan paged_blocks(const calidrop_paged_params* p, int64_t sequences, int64_
 // queries behind 8000 to 32000 rows 813 / 427, 64 queries of 1000 to 16000 rows 541 / 348), so it may cost `ragged` times the
 // other there.  Calls of many blocks level themselves out.
 struct PagedCost { float stream_tile, single, pair, pair_shared; };      // us a tile, alone on a compute unit and in pairs
-PagedPlan plan_paged(const calidrop_paged_params* p, int64_t sequences, int64_t q_len, int64_t max_len) {
+PagedPlan plan_paged(const calidrop_paged_params* p, int64_t total_q, int64_t q_len, int64_t max_len, int64_t shared_len) {
   constexpr PagedCost kCost[2][2] = {{{.4f, 1.05f, 1.33f, 1.4f}, {.6f, 1.35f, 2.1f, 2.25f}}, {{.7f, 1.9f, 2.7f, 2.7f}, {1.2f, 3.f, 5.f, 5.f}}};
   const PagedCost& c = kCost[p->dtype == CALIDROP_FP32][p->head_dim == 128];
-  PagedPlan plan = paged_blocks(p, sequences, q_len, max_len);
-  const int64_t tiles = most_tiles(p, q_len, max_len, plan.rows, plan.tile), groups = plan.items * p->n_kv_heads;
-  if (plan.share == 1 || plan.items > kPagedMostItems || plan.items * tiles >= (int64_t{1} << 31) || groups >= 4 * kPagedTilePlaces) {
+  PagedPlan plan = paged_blocks(p, total_q, q_len, max_len, shared_len);
+  const int64_t tiles = plan.most_tiles, groups = plan.items * p->n_kv_heads;
+  if (plan.share == 1 || plan.items > kPagedMostItems || plan.items * (8 + std::max(tiles, (shared_len + plan.tile - 1) / plan.tile)) >= (int64_t{1} << 31)) {
+    plan.share = 0;
+    return plan;
+  }
+  if (shared_len) return plan;                         // blocks of a long prefix and of short caches: never level
+  if (groups >= 4 * kPagedTilePlaces) {
     plan.share = 0;
     return plan;
   }
@@ -126,7 +135,7 @@ PagedPlan plan_paged(const calidrop_paged_params* p, int64_t sequences, int64_t 
   } else {
     // the queries of a prompt see half of their own rows on average
     const float mean = p->window ? most : std::max(most - .5f * static_cast<float>(q_len) / static_cast<float>(plan.tile), .5f * most);
-    const float places = kPagedTilePlaces, least = static_cast<float>(kPagedLeastRows / plan.tile);
+    const float places = kPagedTilePlaces, least = 2.f;
     const float parts = std::min(places, all * mean / least);
     // as many blocks as places: the long ones end alone
     own = 8.f + (groups <= kPagedTilePlaces / 2 ? c.single * most : groups <= kPagedTilePlaces ? c.pair * mean + c.single * (most - mean)
@@ -134,31 +143,27 @@ PagedPlan plan_paged(const calidrop_paged_params* p, int64_t sequences, int64_t 
     shared = 14.f + 15.f * parts / places * static_cast<float>(plan.rows) / 128.f + c.pair_shared * std::max(mean * all / places, least);
     ragged = groups <= 2 * kPagedTilePlaces ? 1.15f : 1.f;
   }
-  if (shared >= own * (sequences > 1 ? ragged : 1.f)) plan.share = 0;
+  if (shared >= own * (p->batch > 1 ? ragged : 1.f)) plan.share = 0;
   return plan;
 }
 
-// The workspace of a launch: how its blocks were cut, the parts, and with `keep` the whole blocks.
+// The workspace: how blocks were cut, the parts, and with a prefix the whole blocks of both sides.
 struct PagedRegions { size_t cut, part_ml, part_o, whole_ml, whole_o, total; };
-PagedRegions paged_regions(const calidrop_paged_params* p, const PagedPlan& plan, int64_t total_q, bool keep) {
+PagedRegions paged_regions(const calidrop_paged_params* p, const PagedPlan& plan, int64_t total_q) {
   PagedRegions r{};
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += round256(bytes); return here; };
-  const size_t parts = static_cast<size_t>(plan.share) * p->n_kv_heads * 2 * plan.rows, whole = keep ? static_cast<size_t>(total_q) * p->n_q_heads : 0;
+  const size_t parts = static_cast<size_t>(plan.share) * p->n_kv_heads * 2 * plan.rows, whole = plan.prefix ? static_cast<size_t>(total_q) * p->n_q_heads * 2 : 0;
   r.cut = take(static_cast<size_t>(std::min(plan.items, kPagedMostItems)) * sizeof(int4));
   r.part_ml = take(parts * sizeof(float2));
   r.part_o = take(parts * p->head_dim * sizeof(float));
   r.whole_ml = take(whole * sizeof(float2));
   r.whole_o = take(whole * p->head_dim * sizeof(float));
-  r.total = at;
+  r.total = std::max<size_t>(at, 256);
   return r;
 }
-size_t attend_bytes(const calidrop_paged_params* p, int64_t max_q_len, int64_t max_cache_len) {
-  return paged_regions(p, paged_blocks(p, p->batch, max_q_len, max_cache_len), 0, false).total;
-}
-size_t shared_bytes(const calidrop_paged_params* p, int64_t total_q, int64_t max_q_len, int64_t max_cache_len, int64_t shared_len) {
-  return paged_regions(p, paged_blocks(p, p->batch, max_q_len, max_cache_len), total_q, true).total +
-         paged_regions(p, paged_blocks(p, 1, total_q, shared_len), total_q, true).total;
+size_t attend_bytes(const calidrop_paged_params* p, int64_t total_q, int64_t max_q_len, int64_t max_cache_len, int64_t shared_len) {
+  return paged_regions(p, paged_blocks(p, total_q, max_q_len, max_cache_len, shared_len), total_q).total;
 }
 
 int check_attend_sizes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len, int32_t max_cache_len) {
@@ -185,48 +190,29 @@ int check_shared_sizes(const calidrop_paged_params* p, int32_t shared_len) {
 }
 
 template <typename T, int D>
-int launch_paged(const calidrop_paged_params* p, cd::PagedAttendArgs a, const PagedPlan& plan, const PagedRegions& R, char* ws, bool keep,
-                 cd::PagedSide& side, hipStream_t st) {
-  a.blocks = static_cast<int>(plan.blocks); a.items = static_cast<int>(plan.items); a.share = static_cast<int>(plan.share);
-  a.least_tiles = kPagedLeastRows / plan.tile; a.keep = keep;
+int attend_impl(const calidrop_paged_params* p, cd::PagedAttendArgs& a, char* ws, hipStream_t st) {
+  const PagedPlan plan = plan_paged(p, a.total_q, a.max_q_len, a.max_len, a.shared_len);
+  const PagedRegions R = paged_regions(p, plan, a.total_q);
+  a.blocks = static_cast<int>(plan.blocks); a.items = static_cast<int>(plan.items); a.prefix_items = static_cast<int>(plan.prefix);
+  a.share = static_cast<int>(plan.share);
+  a.least_shift = plan.least_shift;
+  a.by_blocks = divisor(a.blocks); a.by_G = divisor(a.G); a.by_Hkv = divisor(p->n_kv_heads);
   a.cut = reinterpret_cast<int4*>(ws + R.cut);
   a.part_ml = reinterpret_cast<float2*>(ws + R.part_ml); a.part_o = reinterpret_cast<float*>(ws + R.part_o);
   a.whole_ml = reinterpret_cast<float2*>(ws + R.whole_ml); a.whole_o = reinterpret_cast<float*>(ws + R.whole_o);
-  side.blocks = a.blocks; side.share = a.share; side.rows = plan.rows; side.cut = a.cut;
-  side.part_o = a.part_o; side.part_ml = a.part_ml; side.whole_o = a.whole_o; side.whole_ml = a.whole_ml;
-  const dim3 grid(static_cast<unsigned>((plan.share ? plan.share : plan.items) * p->n_kv_heads));
   void (*kernel)(cd::PagedAttendArgs);
   if (plan.stream) kernel = plan.share ? cd::paged_stream_kernel<T, D, true> : cd::paged_stream_kernel<T, D, false>;
   else if constexpr (sizeof(T) == 2) kernel = plan.share ? cd::paged_tile_kernel<D, true> : cd::paged_tile_kernel<D, false>;
   else kernel = plan.share ? cd::paged_tile32_kernel<D, true> : cd::paged_tile32_kernel<D, false>;
-  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
-  return launch_status("paged_attend");
-}
-
-// shared_table NULL: no prefix.
-template <typename T, int D>
-int attend_impl(const calidrop_paged_params* p, const cd::PagedAttendArgs& a, const int32_t* shared_table, int32_t shared_len, char* ws,
-                hipStream_t st) {
-  const bool keep = shared_table != nullptr;
-  const PagedPlan own = plan_paged(p, p->batch, a.max_q_len, a.max_len);
-  const PagedRegions own_r = paged_regions(p, own, a.total_q, keep);
-  cd::PagedJoinArgs j{};
-  int rc;
-  if (shared_table) {
-    const PagedPlan prefix = plan_paged(p, 1, a.total_q, shared_len);
-    cd::PagedAttendArgs f = a;
-    f.pages.table = shared_table; f.pages.table_stride = 0; f.lens = nullptr; f.fixed_len = shared_len; f.max_len = shared_len;
-    f.all_see_all = 1; f.batch = 1;
-    if ((rc = launch_paged<T, D>(p, f, prefix, paged_regions(p, prefix, a.total_q, true), ws + own_r.total, true, j.side[1], st))) return rc;
-  }
-  if ((rc = launch_paged<T, D>(p, a, own, own_r, ws, keep, j.side[0], st))) return rc;
-  if (!keep && own.share == 0) return CALIDROP_OK;
-  j.q_off = a.q_off; j.total_q = a.total_q; j.Hq = a.Hq; j.G = a.G; j.Hkv = p->n_kv_heads; j.max_q_len = a.max_q_len; j.out = a.out; j.lse = a.lse;
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>((plan.share ? plan.share : plan.items) * p->n_kv_heads)), dim3(256), 0, st, a);
+  const int rc = launch_status("paged_attend");
+  if (rc || (!plan.prefix && !plan.share)) return rc;
+  cd::PagedJoinArgs j{a, plan.rows};
   const int64_t rows = static_cast<int64_t>(a.max_q_len) * a.G;
-  if (rows * p->n_kv_heads * p->batch >= 4096)
-    hipLaunchKernelGGL((cd::paged_join_kernel<T, D, 1>), dim3(static_cast<unsigned>((rows + 3) / 4), p->n_kv_heads, p->batch), dim3(256), 0, st, j);
-  else
-    hipLaunchKernelGGL((cd::paged_join_kernel<T, D, 4>), dim3(static_cast<unsigned>(rows), p->n_kv_heads, p->batch), dim3(256), 0, st, j);
+  const unsigned Hkv = p->n_kv_heads, nb = p->batch;
+  if (rows * Hkv * nb >= 4096) hipLaunchKernelGGL((cd::paged_join_kernel<T, D, 1>), dim3(static_cast<unsigned>((rows + 3) / 4), Hkv, nb), dim3(256), 0, st, j);
+  else if (rows * Hkv * nb > 256) hipLaunchKernelGGL((cd::paged_join_kernel<T, D, 4>), dim3(static_cast<unsigned>(rows), Hkv, nb), dim3(256), 0, st, j);
+  else hipLaunchKernelGGL((cd::paged_join_kernel<T, D, 16>), dim3(static_cast<unsigned>(rows), Hkv, nb), dim3(1024), 0, st, j);
   return launch_status("paged_join");
 }
 
@@ -249,6 +235,7 @@ int attend_entry(const calidrop_paged_params* p, const void* q, const int32_t* q
   cd::PagedAttendArgs a{};
   a.q = q; a.q_off = q_offsets; a.k = k_pages; a.v = v_pages; a.lens = cache_lens; a.max_len = max_cache_len;
   a.pages = pages_of(p, page_table, p->max_pages);
+  a.shared_table = shared_table; a.shared_len = shared_len;
   a.total_q = total_q; a.batch = p->batch; a.Hq = p->n_q_heads; a.G = p->n_q_heads / p->n_kv_heads;
   a.max_q_len = q_offsets ? max_q_len : 1;
   a.window = std::min(p->window, 1 << 30); a.sinks = std::min(p->sinks, 1 << 30);      // caches have no more rows
@@ -256,7 +243,7 @@ int attend_entry(const calidrop_paged_params* p, const void* q, const int32_t* q
   a.out = out; a.lse = lse;
   hipStream_t st = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
-#define CD_DISPATCH(T, D) return attend_impl<T, D>(p, a, shared_table, shared_len, ws, st)
+#define CD_DISPATCH(T, D) return attend_impl<T, D>(p, a, ws, st)
   if (p->dtype == CALIDROP_BF16) {
     if (p->head_dim == 128) CD_DISPATCH(cd::bf16_t, 128);
     CD_DISPATCH(cd::bf16_t, 64);
@@ -343,7 +330,7 @@ int calidrop_paged_append(const calidrop_paged_params* p, const void* q, int64_t
 
 size_t calidrop_paged_attend_workspace_bytes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len, int32_t max_cache_len) {
   if (check_paged(p) != CALIDROP_OK || check_attend_sizes(p, total_q, max_q_len, max_cache_len) != CALIDROP_OK) return 0;
-  return attend_bytes(p, max_q_len, max_cache_len);
+  return attend_bytes(p, total_q, max_q_len, max_cache_len, 0);
 }
 
 int calidrop_paged_attend(const calidrop_paged_params* p, const void* q, const int32_t* q_offsets, int64_t total_q, int32_t max_q_len,
@@ -353,14 +340,14 @@ int calidrop_paged_attend(const calidrop_paged_params* p, const void* q, const i
   if ((rc = check_paged(p))) return rc;
   if ((rc = check_attend_sizes(p, total_q, max_q_len, max_cache_len))) return rc;
   return attend_entry(p, q, q_offsets, total_q, max_q_len, k_pages, v_pages, nullptr, 0, page_table, cache_lens, max_cache_len, out, lse,
-                      workspace, workspace_bytes, attend_bytes(p, max_q_len, max_cache_len), stream);
+                      workspace, workspace_bytes, attend_bytes(p, total_q, max_q_len, max_cache_len, 0), stream);
 }
 
 size_t calidrop_paged_attend_shared_workspace_bytes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len,
                                                     int32_t max_cache_len, int32_t shared_len) {
   if (check_paged(p) != CALIDROP_OK || check_attend_sizes(p, total_q, max_q_len, max_cache_len) != CALIDROP_OK ||
       check_shared_sizes(p, shared_len) != CALIDROP_OK) return 0;
-  return shared_bytes(p, total_q, max_q_len, max_cache_len, shared_len);
+  return attend_bytes(p, total_q, max_q_len, max_cache_len, shared_len);
 }
 
 int calidrop_paged_attend_shared(const calidrop_paged_params* p, const void* q, const int32_t* q_offsets, int64_t total_q,
@@ -373,7 +360,7 @@ int calidrop_paged_attend_shared(const calidrop_paged_params* p, const void* q, 
   if ((rc = check_shared_sizes(p, shared_len))) return rc;
   if (!shared_table) return fail(CALIDROP_EINVAL, "shared_table is NULL");
   return attend_entry(p, q, q_offsets, total_q, max_q_len, k_pages, v_pages, shared_table, shared_len, page_table, cache_lens,
-                      max_cache_len, out, lse, workspace, workspace_bytes, shared_bytes(p, total_q, max_q_len, max_cache_len, shared_len),
+                      max_cache_len, out, lse, workspace, workspace_bytes, attend_bytes(p, total_q, max_q_len, max_cache_len, shared_len),
                       stream);
 }
 
