@@ -549,12 +549,16 @@ class PagedCache:
     (shapes, types, layouts, the device) and refuses what does not fit with ValueError.
 
     k_pages, v_pages [n_pages][Hkv][page_size][D]; page_table [batch][max_pages] int32; cache_lens [batch] int32.  The tensors
-    stay the caller's: new pages are handed out by writing page_table."""
+    stay the caller's: new pages are handed out by writing page_table.  `p` is copied: later changes of it are not seen."""
 
     def __init__(self, p: PagedParams, k_pages, v_pages, page_table, cache_lens):
-        self.p = p
+        self.p = PagedParams.from_buffer_copy(p)
+        self._p = ctypes.byref(self.p)
+        self.batch, self.n_q_heads, self.n_kv_heads, self.head_dim = p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim
+        self.page_size, self.capacity, self.rot_dim = p.page_size, p.max_pages * p.page_size, p.rot_dim
         self.dtype = torch.bfloat16 if p.dtype == BF16 else torch.float32
         self.device = k_pages.device
+        self._device = k_pages.get_device()                   # its number, -1 for the host
         pages = (p.n_pages, p.n_kv_heads, p.page_size, p.head_dim)
         self._fits(k_pages, "k_pages", self.dtype, pages)
         self._fits(v_pages, "v_pages", self.dtype, pages)
@@ -563,33 +567,36 @@ class PagedCache:
         self.k_pages, self.v_pages, self.page_table, self.cache_lens = k_pages, v_pages, page_table, cache_lens
         self.workspace = None
 
-    def _fits(self, t, name: str, dtype, shape) -> None:
-        if t.shape != shape or t.dtype != dtype or t.device != self.device or not t.is_contiguous():
+    # The checks of a call take as long as its launch, so they ask for little: a device as its number, parameters as plain
+    # attributes (append of single tokens 9.3 us a call with a tensor's device object and the parameters' fields, 7.0 so).
+    def _fits(self, t, name: str, dtype, shape) -> int:
+        if t.shape != shape or t.dtype != dtype or t.get_device() != self._device or not t.is_contiguous():
             raise ValueError(f"{name}: {dtype} {list(shape)} on {self.device}, contiguous, expected, not {t.dtype} "
                              f"{list(t.shape)} on {t.device} with strides {list(t.stride())}")
+        return t.data_ptr()
 
     def _on_device(self, stream) -> Optional[int]:
-        if self.device.type != "cuda" or self.device.index != _raw_device():
+        if self._device < 0 or self._device != _raw_device():
             raise ValueError(f"the cache is on {self.device}, which is not the current device")
         return _stream(stream)
 
     def _heads(self, t, name: str, total: int, heads: int) -> int:
         """Elements between the tokens of q, k or v [total][heads][D]: its heads follow one another, its tokens need not."""
-        d = self.p.head_dim
-        if t.shape != (total, heads, d) or t.dtype != self.dtype or t.device != self.device:
+        d = self.head_dim
+        if t.shape != (total, heads, d) or t.dtype != self.dtype or t.get_device() != self._device:
             raise ValueError(f"{name}: {self.dtype} {[total, heads, d]} on {self.device} expected, not {t.dtype} {list(t.shape)} on {t.device}")
-        stride = t.stride()
-        if stride[2] != 1 or (stride[1] != d and heads > 1):
-            raise ValueError(f"{name}: the heads of a token have to follow one another (strides {list(stride)})")
-        return stride[0] if total > 1 else heads * d
+        to_token, to_head, to_element = t.stride()
+        if to_element != 1 or (to_head != d and heads > 1):
+            raise ValueError(f"{name}: the heads of a token have to follow one another (strides {list(t.stride())})")
+        return to_token if total > 1 else heads * d
 
     def reserve(self, total_q: int, max_q_len: int, max_cache_len: int, shared_len: int = 0) -> None:
-        """A workspace for attention calls of up to these sizes.  Calls that overlap in time (two streams, two captured graphs)
-        need a PagedCache, and with it a workspace, each."""
+        """A workspace for attention calls of up to these sizes, with a prefix of up to shared_len rows.  Calls that overlap in
+        time (two streams, two captured graphs) need a PagedCache, and with it a workspace, each; a captured graph needs the
+        workspace it was captured with, which a larger reservation replaces."""
+        n = calidrop_paged_attend_workspace_bytes(self.p, total_q, max_q_len, max_cache_len)
         if shared_len:
-            n = calidrop_paged_attend_shared_workspace_bytes(self.p, total_q, max_q_len, max_cache_len, shared_len)
-        else:
-            n = calidrop_paged_attend_workspace_bytes(self.p, total_q, max_q_len, max_cache_len)
+            n = max(n, calidrop_paged_attend_shared_workspace_bytes(self.p, total_q, max_q_len, max_cache_len, shared_len))
         if self.workspace is None or self.workspace.nbytes < n:
             self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
 
@@ -597,59 +604,59 @@ class PagedCache:
                stream=None) -> None:
         """k, v [total][Hkv][D] become the next rows of the sequences, rotated on the way; q [total][Hq][D] goes rotated to q_out.
         new_lens None: cache_lens grows in place."""
-        p, total = self.p, k.shape[0]
-        ks = self._heads(k, "k", total, p.n_kv_heads)
-        vs = self._heads(v, "v", total, p.n_kv_heads)
-        qs = 0
+        fits = self._fits
+        total, hkv = k.shape[0], self.n_kv_heads
+        ks, vs, qs = self._heads(k, "k", total, hkv), self._heads(v, "v", total, hkv), 0
         if (q is None) != (q_out is None):
             raise ValueError("q and q_out go together")
+        at_q = at_out = None
         if q is not None:
-            qs = self._heads(q, "q", total, p.n_q_heads)
-            self._fits(q_out, "q_out", self.dtype, (total, p.n_q_heads, p.head_dim))
-        if new_offsets is not None:
-            self._fits(new_offsets, "new_offsets", torch.int32, (p.batch + 1,))
-        if positions is not None:
-            self._fits(positions, "positions", torch.int32, (total,))
-        n_positions = 0
-        if p.rot_dim and rot_table is not None:
+            qs = self._heads(q, "q", total, self.n_q_heads)
+            at_q, at_out = q.data_ptr(), fits(q_out, "q_out", self.dtype, (total, self.n_q_heads, self.head_dim))
+        at_offsets = None if new_offsets is None else fits(new_offsets, "new_offsets", torch.int32, (self.batch + 1,))
+        at_positions = None if positions is None else fits(positions, "positions", torch.int32, (total,))
+        at_table, n_positions = None, 0
+        if rot_table is not None and self.rot_dim:
             n_positions = rot_table.shape[0]
-            self._fits(rot_table, "rot_table", torch.float32, (n_positions, p.rot_dim))
-        if new_lens is None:
-            new_lens = self.cache_lens
-        else:
-            self._fits(new_lens, "new_lens", torch.int32, (p.batch,))
-        calidrop_paged_append(p, q, qs, k, ks, v, vs, new_offsets, total, max_new, positions, rot_table if p.rot_dim else None,
-                              n_positions, self.k_pages, self.v_pages, self.page_table, self.cache_lens, new_lens, q_out,
-                              self._on_device(stream))
+            at_table = fits(rot_table, "rot_table", torch.float32, (n_positions, self.rot_dim))
+        at_lens = self.cache_lens.data_ptr()
+        at_new = at_lens if new_lens is None else fits(new_lens, "new_lens", torch.int32, (self.batch,))
+        _check((_lib or lib()).calidrop_paged_append(
+            self._p, at_q, qs, k.data_ptr(), ks, v.data_ptr(), vs, at_offsets, total, max_new, at_positions, at_table, n_positions,
+            self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.page_table.data_ptr(), at_lens, at_new, at_out,
+            self._on_device(stream)))
 
-    def _queries(self, q, out, lse, q_offsets):
-        p, total = self.p, q.shape[0]
-        shape = (total, p.n_q_heads, p.head_dim)
-        self._fits(q, "q", self.dtype, shape)
-        self._fits(out, "out", self.dtype, shape)
-        self._fits(lse, "lse", torch.float32, shape[:2])
-        if q_offsets is not None:
-            self._fits(q_offsets, "q_offsets", torch.int32, (p.batch + 1,))
-        return total
+    def _attend(self, shared, q, out, lse, q_offsets, max_q_len, max_cache_len, stream) -> None:
+        fits = self._fits
+        total, hq = q.shape[0], self.n_q_heads
+        shape = (total, hq, self.head_dim)
+        at_q, at_out = fits(q, "q", self.dtype, shape), fits(out, "out", self.dtype, shape)
+        at_lse = fits(lse, "lse", torch.float32, (total, hq))
+        at_offsets = None if q_offsets is None else fits(q_offsets, "q_offsets", torch.int32, (self.batch + 1,))
+        if max_cache_len is None:
+            max_cache_len = self.capacity
+        ws = self.workspace
+        at_ws, n_ws = (None, 0) if ws is None else (ws.data_ptr(), ws.nbytes)
+        L = _lib or lib()
+        st = self._on_device(stream)
+        k, v, table, lens = self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.page_table.data_ptr(), self.cache_lens.data_ptr()
+        if shared is None:
+            status = L.calidrop_paged_attend(self._p, at_q, at_offsets, total, max_q_len, k, v, table, lens, max_cache_len, at_out, at_lse,
+                                             at_ws, n_ws, st)
+        else:
+            status = L.calidrop_paged_attend_shared(self._p, at_q, at_offsets, total, max_q_len, k, v, *shared, table, lens, max_cache_len,
+                                                    at_out, at_lse, at_ws, n_ws, st)
+        _check(status)
 
     def attend(self, q, out, lse, q_offsets=None, max_q_len: int = 1, max_cache_len: Optional[int] = None, stream=None) -> None:
         """Attention of the newest tokens, q [total][Hq][D], over the cache, into out and lse [total][Hq]."""
-        total = self._queries(q, out, lse, q_offsets)
-        if max_cache_len is None:
-            max_cache_len = self.p.max_pages * self.p.page_size
-        calidrop_paged_attend(self.p, q, q_offsets, total, max_q_len, self.k_pages, self.v_pages, self.page_table, self.cache_lens,
-                              max_cache_len, out, lse, self.workspace, self._on_device(stream))
+        self._attend(None, q, out, lse, q_offsets, max_q_len, max_cache_len, stream)
 
     def attend_shared(self, q, out, lse, shared_table, shared_len: int, q_offsets=None, max_q_len: int = 1,
                       max_cache_len: Optional[int] = None, stream=None) -> None:
         """The same behind a prefix of shared_len rows in the pages shared_table."""
-        total = self._queries(q, out, lse, q_offsets)
-        if max_cache_len is None:
-            max_cache_len = self.p.max_pages * self.p.page_size
-        self._fits(shared_table, "shared_table", torch.int32, (-(-shared_len // self.p.page_size),))
-        calidrop_paged_attend_shared(self.p, q, q_offsets, total, max_q_len, self.k_pages, self.v_pages, shared_table, shared_len,
-                                     self.page_table, self.cache_lens, max_cache_len, out, lse, self.workspace,
-                                     self._on_device(stream))
+        at = self._fits(shared_table, "shared_table", torch.int32, (-(-shared_len // self.page_size),))
+        self._attend((at, shared_len), q, out, lse, q_offsets, max_q_len, max_cache_len, stream)
 
 
 # ---- device-memory plumbing (allocation only) ----------------------------------------------

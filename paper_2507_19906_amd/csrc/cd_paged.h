@@ -47,6 +47,8 @@ struct PagedAppendArgs {
   Pages pages;
   int64_t total_new;
   int batch, Hq, max_new, max_pages, rot, n_positions, tokens_per_group, write_lens;
+  int units;                                        // of a turned head: pieces of 16 bytes, or pairs of them and single ones
+  Divisor by_units;
 };
 
 // 16 bytes of a row as 32-bit floats, and back.
@@ -72,20 +74,24 @@ template <typename T> __device__ __forceinline__ u32x4 pack16(const float (&f)[E
   return x;
 }
 template <int N> __device__ __forceinline__ void load_floats(const float* p, float (&f)[N]) {
+  typedef float vec __attribute__((ext_vector_type(N < 4 ? N : 4)));
+  constexpr int V = N < 4 ? N : 4;
 #pragma unroll
-  for (int e = 0; e < N; e += 4) {
-    const f32x4 x = *reinterpret_cast<const f32x4*>(p + e);
-    f[e] = x[0]; f[e + 1] = x[1]; f[e + 2] = x[2]; f[e + 3] = x[3];
+  for (int e = 0; e < N; e += V) {
+    const vec x = *reinterpret_cast<const vec*>(p + e);
+#pragma unroll
+    for (int y = 0; y < V; ++y) f[e + y] = x[y];
   }
 }
 
-// A workgroup takes tokens_per_group tokens of one sequence; a thread 16 bytes of one head (two pieces of 16 bytes, the two
-// elements of its pairs, where those lie half the rotated part apart).  The rotation is in 32 bits, rounded once to the
-// storage type.  Bound by the bytes of the heads, read and written once.
+// A workgroup takes tokens_per_group tokens of one sequence, its four waves one token together or one each; a lane 16 bytes of one
+// head (two pieces of 16 bytes, the two elements of its pairs, where those lie half the rotated part apart).  What belongs to a
+// token - its page, its position - is the same in every lane.  The rotation is in 32 bits, rounded once to the storage type.
+// Bound by the bytes of the heads, read and written once.
 template <typename T, int D, bool kHalves>
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
-  constexpr int E = Elem<T>::kPer16B;
-  constexpr int kChunks = D / E;
+  constexpr int E = Elem<T>::kPer16B, kChunks = D / E;
+  constexpr int64_t kRow = D * sizeof(T);
   const int b = blockIdx.y;
   int64_t t0 = b, t1 = b + 1;
   if (a.new_off) { t0 = a.new_off[b]; t1 = a.new_off[b + 1]; }
@@ -94,74 +100,65 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedAppendArgs a) {
   const int n = static_cast<int>(min(t1 - t0, static_cast<int64_t>(a.max_new)));
   const int len = a.lens[b];
   const bool fits = len >= 0 && static_cast<int64_t>(len) + n <= static_cast<int64_t>(a.max_pages) * a.pages.page_size;
-  const int first = static_cast<int>(blockIdx.x) * a.tokens_per_group;
   __syncthreads();                                  // everyone has read the length before it changes
   if (a.write_lens && blockIdx.x == 0 && threadIdx.x == 0) a.new_lens[b] = fits ? len + n : len;
-  const int here = min(a.tokens_per_group, n - first);
-  if (here <= 0) return;
-  const int32_t* table = a.pages.table + b * a.pages.table_stride;
-  const int Hq = a.q ? a.Hq : 0, Hkv = a.pages.Hkv, rot = a.rot;
-  const int turned_units = kHalves ? (D - rot / 2) / E : kChunks;      // threads of a turned head: a pair of pieces, or a piece
-  const int turned = (Hq + Hkv) * turned_units, per_token = turned + Hkv * kChunks;
-  for (int item = threadIdx.x; item < here * per_token; item += 256) {
-    const int tt = item / per_token, r = item - tt * per_token;
-    const int t = first + tt;
-    const int64_t token = t0 + t;
-    const char* src; char* dst;
-    int u; bool turn = false;
-    if (r < turned) {
-      const int h = r / turned_units;
-      u = r - h * turned_units;
-      turn = u < (kHalves ? rot / 2 : rot) / E;
-      if (kHalves && !turn) u += rot / 2 / E;       // the pieces behind the pairs
-      if (h < Hq) {
-        src = a.q + token * a.q_stride + static_cast<int64_t>(h) * D * sizeof(T);
-        dst = a.q_out + (token * Hq + h) * D * sizeof(T);
+  const int wave = wave_index(), lane = threadIdx.x & 63;
+  const bool together = a.tokens_per_group == 1;
+  const int t = static_cast<int>(blockIdx.x) * a.tokens_per_group + (together ? 0 : wave);
+  if (t >= n) return;
+  const int64_t token = t0 + t;
+  const int at = len + t, rot = a.rot, Hkv = a.pages.Hkv;
+  const int first = together ? 64 * wave + lane : lane, step = together ? 256 : 64;
+  const int e = fits ? divide(at, a.pages.div) : 0;
+  const int page = fits ? a.pages.table[b * a.pages.table_stride + e] : -1;
+  const bool stored = page >= 0 && page < a.pages.n_pages;
+  const int64_t slot = stored ? (static_cast<int64_t>(page) * Hkv * a.pages.page_size + (at - e * a.pages.page_size)) * kRow : 0;
+  const int64_t head = a.pages.page_size * kRow;    // from one KV head of a page to the next
+  const float* cs = a.rot_table;
+  if (rot) cs += static_cast<int64_t>(min(max(a.positions ? a.positions[token] : at, 0), a.n_positions - 1)) * rot;
+  const int turned = (kHalves ? rot / 2 : rot) / E;                    // units that turn: a pair of pieces, or a piece
+  auto turn_heads = [&](const char* src, char* dst, int64_t dst_head, int heads) {
+    for (int item = first; item < heads * a.units; item += step) {
+      const int h = divide(item, a.by_units);
+      int u = item - h * a.units;
+      const char* x_at = src + h * kRow;
+      char* to = dst + h * dst_head;
+      if (u >= turned) {
+        if (kHalves) u += turned;                                      // the pieces behind the pairs
+        st16(to + u * 16, ld16_stream(x_at + u * 16));
+      } else if constexpr (kHalves) {
+        const int far = turned * 16;
+        float x[E], y[E], c[E], s[E], p[E], q[E];
+        const u32x4 xb = ld16_stream(x_at + u * 16), yb = ld16_stream(x_at + u * 16 + far);
+        load_floats(cs + u * E, c);
+        load_floats(cs + rot / 2 + u * E, s);
+        unpack16<T>(xb, x);
+        unpack16<T>(yb, y);
+#pragma unroll
+        for (int i = 0; i < E; ++i) { p[i] = x[i] * c[i] - y[i] * s[i]; q[i] = y[i] * c[i] + x[i] * s[i]; }
+        st16(to + u * 16, pack16<T>(p));
+        st16(to + u * 16 + far, pack16<T>(q));
       } else {
-        src = a.k + token * a.k_stride + static_cast<int64_t>(h - Hq) * D * sizeof(T);
-        dst = a.k_pages;
-      }
-      if (h >= Hq) {
-        if (!fits) continue;
-        const int e = divide(len + t, a.pages.div), page = table[e];
-        if (page < 0 || page >= a.pages.n_pages) continue;
-        dst += ((static_cast<int64_t>(page) * Hkv + (h - Hq)) * a.pages.page_size + (len + t - e * a.pages.page_size)) * D * sizeof(T);
-      }
-    } else {
-      const int h = (r - turned) / kChunks;
-      u = (r - turned) - h * kChunks;
-      if (!fits) continue;
-      const int e = divide(len + t, a.pages.div), page = table[e];
-      if (page < 0 || page >= a.pages.n_pages) continue;
-      src = a.v + token * a.v_stride + static_cast<int64_t>(h) * D * sizeof(T);
-      dst = a.v_pages + ((static_cast<int64_t>(page) * Hkv + h) * a.pages.page_size + (len + t - e * a.pages.page_size)) * D * sizeof(T);
-    }
-    if (!turn) { st16(dst + u * 16, ld16(src + u * 16)); continue; }
-    const int pos = min(max(a.positions ? a.positions[token] : len + t, 0), a.n_positions - 1);
-    const float* cs = a.rot_table + static_cast<int64_t>(pos) * rot;
-    if constexpr (kHalves) {
-      const int far = rot / 2 * static_cast<int>(sizeof(T));
-      float x[E], y[E], c[E], s[E], p[E], q[E];
-      unpack16<T>(ld16(src + u * 16), x);
-      unpack16<T>(ld16(src + u * 16 + far), y);
-      load_floats(cs + u * E, c);
-      load_floats(cs + rot / 2 + u * E, s);
+        float x[E], c[E / 2], s[E / 2], p[E];
+        const u32x4 xb = ld16_stream(x_at + u * 16);
+        load_floats(cs + u * (E / 2), c);
+        load_floats(cs + rot / 2 + u * (E / 2), s);
+        unpack16<T>(xb, x);
 #pragma unroll
-      for (int e = 0; e < E; ++e) { p[e] = x[e] * c[e] - y[e] * s[e]; q[e] = y[e] * c[e] + x[e] * s[e]; }
-      st16(dst + u * 16, pack16<T>(p));
-      st16(dst + u * 16 + far, pack16<T>(q));
-    } else {
-      float x[E], p[E];
-      unpack16<T>(ld16(src + u * 16), x);
-#pragma unroll
-      for (int e = 0; e < E / 2; ++e) {
-        const float c = cs[u * (E / 2) + e], s = cs[rot / 2 + u * (E / 2) + e];
-        p[2 * e] = x[2 * e] * c - x[2 * e + 1] * s;
-        p[2 * e + 1] = x[2 * e + 1] * c + x[2 * e] * s;
+        for (int i = 0; i < E / 2; ++i) {
+          p[2 * i] = x[2 * i] * c[i] - x[2 * i + 1] * s[i];
+          p[2 * i + 1] = x[2 * i + 1] * c[i] + x[2 * i] * s[i];
+        }
+        st16(to + u * 16, pack16<T>(p));
       }
-      st16(dst + u * 16, pack16<T>(p));
     }
-  }
+  };
+  if (a.q) turn_heads(a.q + token * a.q_stride, a.q_out + token * a.Hq * kRow, kRow, a.Hq);
+  if (!stored) return;
+  turn_heads(a.k + token * a.k_stride, a.k_pages + slot, head, Hkv);
+  const char* v = a.v + token * a.v_stride;
+  for (int item = first; item < Hkv * kChunks; item += step)
+    st16(a.v_pages + slot + item / kChunks * head + item % kChunks * 16, ld16_stream(v + item * 16));
 }
 
 // new_lens of calls whose sequences have several workgroups, where it is the array the lengths are read from.

@@ -310,6 +310,8 @@ int calidrop_paged_append(const calidrop_paged_params* p, const void* q, int64_t
   a.total_new = total_new; a.batch = p->batch; a.Hq = p->n_q_heads; a.max_new = new_offsets ? max_new : 1;
   a.max_pages = p->max_pages; a.rot = p->rot_dim; a.n_positions = n_positions;
   a.tokens_per_group = a.max_new == 1 ? 1 : 4;
+  a.units = (p->rot_pairs == CALIDROP_ROT_HALVES ? p->head_dim - p->rot_dim / 2 : p->head_dim) * elem / 16;
+  a.by_units = divisor(a.units);
   const int groups = ceil_div(a.max_new, a.tokens_per_group);
   a.write_lens = groups == 1 || new_lens != cache_lens;
   const dim3 grid(groups, p->batch);
