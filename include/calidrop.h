@@ -449,8 +449,8 @@ int calidrop_recalibrate_packed(const calidrop_params* p, const void* q_t, const
  * result meaningless.  K and V rows that a query of a call sees must be finite; what other rows hold does not matter.
  *
  * Tokens of a call are packed: those of sequence b are offsets[b] .. offsets[b+1]-1 (any number, none included), where NULL
- * offsets mean one token per sequence (then the total must be batch).  Tokens that no sequence owns (behind the last one)
- * are neither read nor written.
+ * offsets mean one token per sequence (then the total must be batch).  For tokens that no sequence owns (behind the last one)
+ * nothing is written.  A workspace holds a call's partial results while it runs: calls that overlap in time need one each.
  */
 typedef enum {
   CALIDROP_ROT_HALVES = 0,     /* element j of the rotated part is paired with element j + rot_dim / 2 */
@@ -464,7 +464,7 @@ typedef struct {
   int32_t n_q_heads, n_kv_heads, head_dim; /* as in calidrop_params                           */
   int32_t page_size;    /* rows of a page, any number >= 1                                    */
   int32_t n_pages;      /* pages in k_pages and in v_pages; n_pages * Hkv * page_size < 2^32  */
-  int32_t max_pages;    /* entries of a sequence in page_table                                */
+  int32_t max_pages;    /* entries of a sequence in page_table; max_pages * page_size < 2^31  */
   float scale;          /* logit scale; 0 selects 1/sqrt(D)                                   */
   int32_t window;       /* attention: 0 = a query sees every row up to its own; W >= 1 = its own and
                            the W - 1 rows before it                                           */

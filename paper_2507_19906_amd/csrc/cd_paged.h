@@ -246,7 +246,7 @@ struct PagedBlock {
   static constexpr int kSetup = kRows == 16 ? 4 : 3;
   int R, r0, len, past;      // past: row of the first query, len in a prefix
   bool prefix;
-  int64_t q0;
+  int64_t q0;                // first token
   const int32_t* table;
   KeyTiles<TK> kt;
   __device__ __forceinline__ void init(const PagedAttendArgs& a, int item) {
@@ -547,11 +547,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void paged_stream_kern
     const int r = blk.r0 + i;
     const bool valid = r < blk.R;
     const int t = valid ? divide(r, a.by_G) : 0;
-    const int64_t row = (blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);     // where valid
+    const int row = static_cast<int>(blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);     // where valid; below 2^30
     const int pos = valid ? blk.pos_of(a, r) : -1;
     W w;
     w.clear();
-    w.load_q(0, static_cast<const T*>(a.q) + (valid ? row : 0) * D, valid, c);
+    w.load_q(0, static_cast<const T*>(a.q) + static_cast<int64_t>(valid ? row : 0) * D, valid, c);
     auto row_of = [&](int u) -> uint32_t {                   // of row lane % 32 of the tile
       int base, from, to;
       blk.kt.tile(u, base, from, to);
@@ -724,12 +724,12 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
     const int wr0 = blk.r0 + 32 * wave, r = wr0 + col;
     const bool valid = r < blk.R, any_rows = wr0 < blk.R;
     const int t = valid ? divide(r, a.by_G) : 0;
-    const int64_t row = (blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);       // where valid
+    const int row = static_cast<int>(blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);       // where valid; below 2^30
     const int pos = valid ? blk.pos_of(a, r) : -1;
     const int wave_min = blk.pos_of(a, wr0), wave_max = blk.pos_of(a, min(wr0 + 32, blk.R) - 1);
     u32x4 qf[NS];
 #pragma unroll
-    for (int st = 0; st < NS; ++st) qf[st] = valid ? ld16(static_cast<const uint16_t*>(a.q) + row * D + st * 16 + h * 8) : zero16();
+    for (int st = 0; st < NS; ++st) qf[st] = valid ? ld16(static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(row) * D + st * 16 + h * 8) : zero16();
     f32x16 o[ND];
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -854,7 +854,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
     if (!valid) return;
     if (to.final_rows) {
       const float inv = l > 0.f ? 1.f / l : 0.f;
-      uint16_t* out = static_cast<uint16_t*>(a.out) + row * D;
+      uint16_t* out = static_cast<uint16_t*>(a.out) + static_cast<int64_t>(row) * D;
 #pragma unroll
       for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -895,11 +895,11 @@ __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a)
     const int wave_max = blk.pos_of(a, min(wr0 + 16, blk.R) - 1);
     const bool valid = r < blk.R;
     const int t0 = valid ? divide(r, a.by_G) : 0;
-    const int64_t row = (blk.q0 + t0) * a.Hq + g * a.G + (r - t0 * a.G);     // where valid
+    const int row = static_cast<int>(blk.q0 + t0) * a.Hq + g * a.G + (r - t0 * a.G);     // where valid; below 2^30
     const int pos = valid ? blk.pos_of(a, r) : -1;
     W w;
     w.clear();
-    w.load_q(0, static_cast<const float*>(a.q) + (valid ? row : 0) * D, valid, c);
+    w.load_q(0, static_cast<const float*>(a.q) + static_cast<int64_t>(valid ? row : 0) * D, valid, c);
     P tiles{a, blk.table, g, wave, lane, 0, 0};
     const int u_end = min(u1, blk.kt.n);
     auto step = [&](int u, const char* __restrict kc, const char* __restrict vc, char* __restrict kn, char* __restrict vn) __attribute__((always_inline)) {

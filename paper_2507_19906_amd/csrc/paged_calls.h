@@ -25,6 +25,8 @@ int check_paged(const calidrop_paged_params* p) {
     return fail(CALIDROP_EINVAL, "page_size, n_pages and max_pages must be >= 1 (got %d, %d, %d)", p->page_size, p->n_pages, p->max_pages);
   if (static_cast<double>(p->page_size) * p->n_pages * p->n_kv_heads >= 4294967296.0)
     return fail(CALIDROP_EUNSUPPORTED, "n_pages * n_kv_heads * page_size exceeds 2^32 rows");
+  if (static_cast<int64_t>(p->max_pages) * p->page_size > INT32_MAX)
+    return fail(CALIDROP_EUNSUPPORTED, "max_pages * page_size exceeds 2^31 - 1 rows");
   if (!(p->scale >= 0.f) || std::isinf(p->scale))
     return fail(CALIDROP_EINVAL, "scale must be finite and >= 0 (0 selects 1/sqrt(head_dim))");
   if (p->window < 0 || p->sinks < 0)
@@ -174,8 +176,8 @@ int check_attend_sizes(const calidrop_paged_params* p, int64_t total_q, int32_t 
     return fail(CALIDROP_EUNSUPPORTED, "total_q * n_q_heads exceeds 2^30");
   const int64_t G = p->n_q_heads / p->n_kv_heads;
   if (max_q_len > (1 << 26) / G) return fail(CALIDROP_EUNSUPPORTED, "max_q_len * (n_q_heads / n_kv_heads) exceeds 2^26");
-  if ((max_q_len * G + 127) / 128 * p->n_kv_heads * p->batch >= 1 << 24)        // workgroups of 256 threads on one grid axis
-    return fail(CALIDROP_EUNSUPPORTED, "batch * max_q_len * n_q_heads exceeds 2^31");
+  if ((max_q_len * G + 63) / 64 * p->n_kv_heads * p->batch >= 1 << 24)          // workgroups of 256 threads on one grid axis
+    return fail(CALIDROP_EUNSUPPORTED, "batch * max_q_len * n_q_heads exceeds 2^30");
   if (max_cache_len > paged_capacity(p))
     return fail(CALIDROP_ESHAPE, "max_cache_len %d exceeds the max_pages * page_size = %lld rows of a table", max_cache_len,
                 static_cast<long long>(paged_capacity(p)));
@@ -273,7 +275,7 @@ int calidrop_paged_append(const calidrop_paged_params* p, const void* q, int64_t
   if ((rc = check_paged(p))) return rc;
   if (total_new < 0 || max_new < 1)
     return fail(CALIDROP_ESHAPE, "total_new >= 0 and max_new >= 1 expected (got %lld, %d)", static_cast<long long>(total_new), max_new);
-  if (total_new > (int64_t{1} << 30)) return fail(CALIDROP_EUNSUPPORTED, "total_new exceeds 2^30");
+  if (total_new > (int64_t{1} << 30) || max_new > (1 << 25)) return fail(CALIDROP_EUNSUPPORTED, "total_new exceeds 2^30 or max_new 2^25");
   if (!new_offsets && total_new != p->batch)
     return fail(CALIDROP_ESHAPE, "without new_offsets every sequence has one token: total_new %lld is not the batch %d",
                 static_cast<long long>(total_new), p->batch);

@@ -74,13 +74,14 @@ class Setup:
         self.out = torch.full((self.total, hq, d), 77.0, dtype=dt, device=DEV)
         self.lse = torch.full((self.total, hq), 77.0, device=DEV)
         self.q_off = None if one else ints(self.offs)
+        self.shared_table = ints(self.shared)
         self.most = dict(max_q_len=max(1, max(nq)), max_cache_len=max(lens))
         self.cache.reserve(self.total, self.most["max_q_len"], self.most["max_cache_len"], prefix)
         self.cache.workspace.fill_(255)                     # NaN partials wherever a call reads what it has not written
 
     def run(self, stream=None):
         if self.prefix:
-            self.cache.attend_shared(self.qd, self.out, self.lse, ints(self.shared), self.prefix, q_offsets=self.q_off, stream=stream, **self.most)
+            self.cache.attend_shared(self.qd, self.out, self.lse, self.shared_table, self.prefix, q_offsets=self.q_off, stream=stream, **self.most)
         else:
             self.cache.attend(self.qd, self.out, self.lse, q_offsets=self.q_off, stream=stream, **self.most)
         return self
@@ -228,6 +229,50 @@ def test_the_prefix_equals_one_cache_each():
     # both within the bound of the exact result, 2^-8 A + 2^-8 |out| and small terms; A < 4 for normal v (a mean of |v|)
     assert (out.float() - s.out.float()).abs().max() < 2 * (4 + 4) * 2.0 ** -8
     assert (lse - s.lse).abs().max() < 1e-4
+
+
+@pytest.mark.parametrize("prefix", [0, 70])
+@pytest.mark.parametrize("nb,nq,hq,hkv,dtype", [(5000, 1, 2, 1, "bf16"), (4500, 20, 2, 1, "bf16"), (3, 1, 800, 800, "fp32"), (2, 40, 520, 520, "bf16"),
+                                                (2, 1, 2000, 125, "bf16")])
+def test_many_sequences_and_many_heads(prefix, nb, nq, hq, hkv, dtype):
+    # more blocks than are added up on the device, more KV heads than workgroups to share them: a workgroup per block
+    lens = [nq + (b * 37) % 50 for b in range(nb)]
+    Setup(lens, [nq] * nb, hq, hkv, 64, dtype, 32, prefix=prefix, seed=15).run().check(range(0, nb, max(1, nb // 4)) if hq < 100 else [0])
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_both_forms_of_a_call(dtype, d):
+    # one launch where every block has a workgroup, two where workgroups share the tiles
+    def launches(lens, nq, **kw):
+        s = Setup(lens, nq, 8, 2, d, dtype, 32, seed=16, **kw)
+        n = len(H.captured_launches(lambda: s.run()))
+        s.run().check([0])
+        return n
+    assert launches([90] * 70, [1] * 70, one=True) == 1 and launches([3000], [1], one=True) == 2
+    assert launches([100] * 3, [100] * 3) == 1 and launches([6000], [40]) == 2
+    assert launches([50, 3], [1, 1], one=True, prefix=300) == 2
+
+
+def test_lengths_that_cannot_be():
+    # below zero: no rows; above what the host was told: cut off there, the queries ending at the cut
+    s = Setup([40, 70, 90], [2, 1, 3], 8, 2, 64, "bf16", 16, seed=17)
+    s.cache.cache_lens.copy_(ints([-5, 70, 1 << 30]))
+    s.run()
+    torch.cuda.synchronize()
+    assert (s.out[:2] == 0).all() and (s.lse[:2] == -math.inf).all()
+    s.check([1, 2])                                         # max_cache_len is 90
+
+
+def test_offsets_that_cannot_be():
+    # falling, and beyond the tokens: what is in range is computed, nothing else is touched
+    s = Setup([40, 70, 90], [2, 1, 3], 8, 2, 64, "bf16", 16, seed=18, spare_tokens=2)
+    s.q_off = ints([0, 2, 1, 1 << 30])
+    s.run()
+    torch.cuda.synchronize()
+    got = s.out[:2].clone()
+    s.q_off = ints(s.offs)
+    s.run().check()
+    assert torch.equal(got[:1], s.out[:1])
 
 
 # ---- append -------------------------------------------------------------------------------------------------------------------

@@ -107,6 +107,7 @@ BAD_PARAMS = [
     (dict(dtype=2), cd.EUNSUPPORTED), (dict(batch=0), cd.EINVAL), (dict(batch=65536), cd.EUNSUPPORTED), (dict(n_q_heads=0), cd.EINVAL),
     (dict(n_q_heads=33), cd.ESHAPE), (dict(n_q_heads=17, n_kv_heads=1), cd.EUNSUPPORTED), (dict(head_dim=96), cd.EUNSUPPORTED),
     (dict(page_size=0), cd.EINVAL), (dict(n_pages=0), cd.EINVAL), (dict(max_pages=0), cd.EINVAL), (dict(n_pages=1 << 25), cd.EUNSUPPORTED),
+    (dict(max_pages=1 << 27), cd.EUNSUPPORTED),
     (dict(scale=-1.0), cd.EINVAL), (dict(scale=float("nan")), cd.EINVAL), (dict(scale=float("inf")), cd.EINVAL), (dict(window=-1), cd.EINVAL),
     (dict(sinks=-1), cd.EINVAL), (dict(rot_dim=-16), cd.EINVAL), (dict(rot_dim=144), cd.EINVAL), (dict(rot_dim=24), cd.EUNSUPPORTED),
     (dict(rot_pairs=2), cd.EINVAL)]
@@ -163,7 +164,8 @@ def test_foreign_struct_sizes_are_refused():
                                                                            "new_lens", "q_out", "new_offsets", "positions", "rot_table")],
     ("calidrop_paged_append", append_args, dict(total_new=-1), cd.ESHAPE), ("calidrop_paged_append", append_args, dict(max_new=0), cd.ESHAPE),
     ("calidrop_paged_append", append_args, dict(new_offsets=None), cd.ESHAPE), ("calidrop_paged_append", append_args, dict(n_positions=0), cd.ESHAPE),
-    ("calidrop_paged_append", append_args, dict(total_new=(1 << 30) + 1), cd.EUNSUPPORTED),
+    ("calidrop_paged_append", append_args, dict(total_new=(1 << 30) + 1), cd.EUNSUPPORTED), ("calidrop_paged_append", append_args, dict(max_new=(1 << 25) + 1), cd.EUNSUPPORTED),
+    *[(c, a, dict(max_q_len=1 << 25), cd.EUNSUPPORTED) for c, a in CALLS[1:]],
     ("calidrop_paged_append", append_args, dict(q_stride=4095), cd.ESHAPE), ("calidrop_paged_append", append_args, dict(k_stride=1023), cd.ESHAPE),
     ("calidrop_paged_append", append_args, dict(v_stride=1025), cd.EALIGN), ("calidrop_paged_append", append_args, dict(q_out=A, q_stride=5120), cd.ESHAPE),
     *[("calidrop_paged_attend", attend_args, {n: None}, cd.EINVAL) for n in ("q", "k_pages", "v_pages", "page_table", "cache_lens", "out", "lse")],
