@@ -788,6 +788,18 @@ class CompressBuffers:
                              self.indices, self.cal_indices, self.flags, self.a_lse, self.out, self.c_q,
                              self.c_out, self.c_lse, self.ws_recal, stream)
 
+    def paged(self, **kw) -> "PagedCache":
+        """The compressed caches as pages of their capacity, one per sequence (uniform capacities): rows rotated and appended to
+        them, attention over them without calibration.  `kw`: rot_dim, rot_pairs, window, sinks of make_paged_params."""
+        if not self.uniform:
+            raise ValueError("only caches of one capacity are pages")
+        p, nb = self.p, self.p.batch
+        shape = (nb, p.n_kv_heads, self.cap, p.head_dim)
+        pp = make_paged_params(dtype=p.dtype, batch=nb, n_q_heads=p.n_q_heads, n_kv_heads=p.n_kv_heads, head_dim=p.head_dim,
+                               page_size=self.cap, n_pages=nb, max_pages=1, scale=p.scale, **kw)
+        table = torch.arange(nb, dtype=torch.int32, device=self.out.device).view(nb, 1)
+        return PagedCache(pp, self.k_c.view(shape), self.v_c.view(shape), table, self.cache_lens)
+
     def region(self, region: int) -> torch.Tensor:
         off, nbytes = calidrop_compress_workspace_region(self.p, self.total_tokens,
                                                          self.max_seq_len, region)

@@ -401,11 +401,10 @@ __device__ __forceinline__ void paged_blocks(const PagedAttendArgs& a, PagedShar
   }
 }
 
-// Few queries, up to 16 (token, head) rows: the 4 waves of a workgroup take its 32-row tiles in turn.  S^T = K Q^T on the matrix cores puts a query into a column,
-// so that its softmax weights stay in the lanes that made them and are the B operand of O^T += V^T P^T as they are: the rows
-// of a tile are dealt to the K operand in the order in which the products want the weights.  K and V go from memory to
-// registers without LDS.  Bound by the bytes of K and V.
-template <typename T, int D, int NT>
+// A wave with 16 (token, head) rows, in the layout of the 16 x 16 products (lane l = 16 c + i).  S^T = K Q^T puts a query into a
+// column, so that its softmax weights stay in the lanes that made them and are the B operand of O^T += V^T P^T as they are: the
+// rows of a tile are dealt to the K operand in the order in which the products want the weights.
+template <typename T, int D>
 struct PagedWave {
   static constexpr int EPL = Elem<T>::kPer16B, KD = Elem<T>::kStepK, NK = D / KD;
   static constexpr bool kBf16 = sizeof(T) == 2;
@@ -414,35 +413,32 @@ struct PagedWave {
   static constexpr int NACC = NP * NX;                     // O^T tiles: 16 rows (slots of D) x 16 queries
   typedef uint32_t VPiece __attribute__((ext_vector_type(kBf16 && D == 64 ? 2 : 4)));
 
-  u32x4 qf[NT][NK];
-  f32x4 o[NT][NACC];
-  float m[NT], l[NT];                                      // running maximum (log2 units) and this lane's share of the sum
+  u32x4 qf[NK];
+  f32x4 o[NACC];
+  float m, l;                                      // running maximum (log2 units) and this lane's share of the sum
 
   // row of a tile that lane (i, c) loads for K group t, and for slot e of V
   static __device__ __forceinline__ int k_row(int t, int i) { return kBf16 ? 8 * (i >> 2) + 4 * t + (i & 3) : 16 * t + i; }
   static __device__ __forceinline__ int v_row(int e, int c) { return kBf16 ? 8 * c + e : 16 * (e >> 2) + 4 * c + (e & 3); }
   // row of a tile of weight r of K group t in lane group c
   static __device__ __forceinline__ int p_row(int t, int c, int r) { return kBf16 ? 8 * c + 4 * t + r : 16 * t + 4 * c + r; }
-  // first of the elements of D that lane group c holds of output piece p: o[.][p NX + x][r] is element d_first + r NX + x
+  // first of the elements of D that lane group c holds of output piece p: o[p NX + x][r] is element d_first + r NX + x
   static __device__ __forceinline__ int d_first(int p, int c) { return p * 64 + c * 4 * NX; }
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int x = 0; x < NACC; ++x) o[nt][x] = f32x4{0.f, 0.f, 0.f, 0.f};
-      m[nt] = -INFINITY;
-      l[nt] = 0.f;
-    }
+    for (int x = 0; x < NACC; ++x) o[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
   }
-  __device__ __forceinline__ void load_q(int nt, const T* q, bool valid, int c) {
+  __device__ __forceinline__ void load_q(const T* q, bool valid, int c) {
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk) qf[nt][kk] = valid ? ld16(q + kk * KD + c * EPL) : zero16();
+    for (int kk = 0; kk < NK; ++kk) qf[kk] = valid ? ld16(q + kk * KD + c * EPL) : zero16();
   }
   // Logits to weights: s[x] are those of K group t0 + x of the tile at `base`; sums and outputs so far are rescaled to the new
   // maximum.
   template <int N>
-  __device__ __forceinline__ void weigh(int nt, f32x4* s, int t0, int base, int from, int to, int pos, const PagedAttendArgs& a, int c) {
+  __device__ __forceinline__ void weigh(f32x4* s, int t0, int base, int from, int to, int pos, const PagedAttendArgs& a, int c) {
     float top = -INFINITY;
 #pragma unroll
     for (int t = 0; t < N; ++t)
@@ -453,38 +449,38 @@ struct PagedWave {
         s[t][r] = see ? s[t][r] * a.sl2 : -INFINITY;
         top = fmaxf(top, s[t][r]);
       }
-    const float mn = fmaxf(m[nt], col4_max(top));
+    const float mn = fmaxf(m, col4_max(top));
     const float ref = mn == -INFINITY ? 0.f : mn;
-    const float f = mn == m[nt] ? 1.f : fast_exp2(m[nt] - ref);
-    m[nt] = mn;
+    const float f = mn == m ? 1.f : fast_exp2(m - ref);
+    m = mn;
     float sum = 0.f;
 #pragma unroll
     for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) { s[t][r] = fast_exp2(s[t][r] - ref); sum += s[t][r]; }
-    l[nt] = l[nt] * f + sum;
+    l = l * f + sum;
     if (__any(f != 1.f)) {
 #pragma unroll
-      for (int x = 0; x < NACC; ++x) o[nt][x] *= f;
+      for (int x = 0; x < NACC; ++x) o[x] *= f;
     }
   }
-  // The results of column nt, block row `br`, (token, head) row `row`; l is the whole sum.
-  __device__ __forceinline__ void write(int nt, const PagedTarget& to, const PagedAttendArgs& a, int64_t row, int br, int c) const {
+  // The results of this lane's column, block row `br`, (token, head) row `row`; l is the whole sum.
+  __device__ __forceinline__ void write(const PagedTarget& to, const PagedAttendArgs& a, int64_t row, int br, int c) const {
     if (to.final_rows) {
-      const float inv = l[nt] > 0.f ? 1.f / l[nt] : 0.f;
+      const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
       for (int p = 0; p < NP; ++p)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
           for (int x = 0; x < NX; ++x)
-            store_elem(static_cast<T*>(a.out), row * D + d_first(p, c) + r * NX + x, o[nt][p * NX + x][r] * inv);
-      if (c == 0) a.lse[row] = l[nt] > 0.f ? (m[nt] + fast_log2(l[nt])) * kLn2 : -INFINITY;
+            store_elem(static_cast<T*>(a.out), row * D + d_first(p, c) + r * NX + x, o[p * NX + x][r] * inv);
+      if (c == 0) a.lse[row] = l > 0.f ? (m + fast_log2(l)) * kLn2 : -INFINITY;
       return;
     }
     const int64_t at = to.by_row ? row : br;
-    if (c == 0) to.ml[at] = float2{m[nt], l[nt]};
-    if (l[nt] == 0.f) return;
+    if (c == 0) to.ml[at] = float2{m, l};
+    if (l == 0.f) return;
 #pragma unroll
     for (int p = 0; p < NP; ++p)
 #pragma unroll
@@ -492,7 +488,7 @@ struct PagedWave {
 #pragma unroll
         for (int x = 0; x < NX; x += 4)
           *reinterpret_cast<f32x4*>(to.o + at * D + d_first(p, c) + r * NX + x) =
-              f32x4{o[nt][p * NX + x][r], o[nt][p * NX + x + 1][r], o[nt][p * NX + x + 2][r], o[nt][p * NX + x + 3][r]};
+              f32x4{o[p * NX + x][r], o[p * NX + x + 1][r], o[p * NX + x + 2][r], o[p * NX + x + 3][r]};
   }
 
   __device__ __forceinline__ void load_k(const T* k, uint32_t rid, int i, int c, u32x4 (&kf)[2][NK]) const {
@@ -528,11 +524,17 @@ struct PagedWave {
   }
 };
 
+// Few queries, up to 16 (token, head) rows: the 4 waves of a workgroup take its 32-row tiles in turn, K and V from memory to
+// registers without LDS, the page of the next tile's rows looked up by one lane each meanwhile.
+// Bound by the bytes of K and V: 64 sequences of 16001 rows, D = 128 in bf16, 32 query and 8 KV heads, 667 us, 6.3 TB/s; of 1000
+// to 16000 rows 348 us, 6.1 TB/s; one of 32768 rows 25 us and 5 for the launch that joins the parts, 4.1 TB/s together.  Tried
+// and no faster: K and V of a tile requested while the one before is worked on (31.3 for 32.2 us, fp32 121 for 107), 512, 640
+// or 1024 places for shares instead of 768 (bf16: three workgroups on a compute unit).
 constexpr int kStreamRows = 16, kStreamTile = 32;
 
 template <typename T, int D, bool kShare>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void paged_stream_kernel(PagedAttendArgs a) {
-  using W = PagedWave<T, D, 1>;
+  using W = PagedWave<T, D>;
   constexpr int TK = kStreamTile, kWaves = 4;
   __shared__ f32x4 so[2][W::NACC][64];
   __shared__ float sm[2][64], sl[2][64];
@@ -551,7 +553,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void paged_stream_kern
     const int pos = valid ? blk.pos_of(a, r) : -1;
     W w;
     w.clear();
-    w.load_q(0, static_cast<const T*>(a.q) + static_cast<int64_t>(valid ? row : 0) * D, valid, c);
+    w.load_q(static_cast<const T*>(a.q) + static_cast<int64_t>(valid ? row : 0) * D, valid, c);
     auto row_of = [&](int u) -> uint32_t {                   // of row lane % 32 of the tile
       int base, from, to;
       blk.kt.tile(u, base, from, to);
@@ -573,45 +575,45 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void paged_stream_kern
 #pragma unroll
       for (int kk = 0; kk < W::NK; ++kk)
 #pragma unroll
-        for (int t2 = 0; t2 < 2; ++t2) mma_step<T>(sc[t2], kf[t2][kk], w.qf[0][kk]);
-      w.template weigh<2>(0, sc, 0, base, from, to, pos, a, c);
+        for (int t2 = 0; t2 < 2; ++t2) mma_step<T>(sc[t2], kf[t2][kk], w.qf[kk]);
+      w.template weigh<2>(sc, 0, base, from, to, pos, a, c);
       // The weights are rounded to the type of V, the precision the matrix cores take them in.
       if constexpr (W::kBf16) {
         const u32x4 pf = {pack_bf16x2(sc[0][0], sc[0][1]), pack_bf16x2(sc[0][2], sc[0][3]), pack_bf16x2(sc[1][0], sc[1][1]), pack_bf16x2(sc[1][2], sc[1][3])};
 #pragma unroll
-        for (int x = 0; x < W::NX; ++x) mma_step<T>(w.o[0][x], w.v_operand(vf, 0, x, 0), pf);
+        for (int x = 0; x < W::NX; ++x) mma_step<T>(w.o[x], w.v_operand(vf, 0, x, 0), pf);
       } else {
 #pragma unroll
         for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
           for (int p = 0; p < W::NP; ++p)
 #pragma unroll
-            for (int x = 0; x < W::NX; ++x) mma_step<T>(w.o[0][p * W::NX + x], w.v_operand(vf, p, x, t2), __builtin_bit_cast(u32x4, sc[t2]));
+            for (int x = 0; x < W::NX; ++x) mma_step<T>(w.o[p * W::NX + x], w.v_operand(vf, p, x, t2), __builtin_bit_cast(u32x4, sc[t2]));
       }
     }
     // The four waves' shares, joined pairwise through LDS: (2, 3) into (0, 1), then 1 into 0.
-    w.l[0] = col4_sum(w.l[0]);
+    w.l = col4_sum(w.l);
 #pragma unroll
     for (int half = 2; half >= 1; half >>= 1) {
       if (wave >= half && wave < 2 * half) {
 #pragma unroll
-        for (int x = 0; x < W::NACC; ++x) so[wave - half][x][lane] = w.o[0][x];
-        sm[wave - half][lane] = w.m[0];
-        sl[wave - half][lane] = w.l[0];
+        for (int x = 0; x < W::NACC; ++x) so[wave - half][x][lane] = w.o[x];
+        sm[wave - half][lane] = w.m;
+        sl[wave - half][lane] = w.l;
       }
       __syncthreads();
       if (wave < half) {
-        const float m2 = sm[wave][lane], mn = fmaxf(w.m[0], m2), ref = mn == -INFINITY ? 0.f : mn;
-        const float f = fast_exp2(w.m[0] - ref), f2 = fast_exp2(m2 - ref);
-        w.m[0] = mn;
-        w.l[0] = w.l[0] * f + sl[wave][lane] * f2;
+        const float m2 = sm[wave][lane], mn = fmaxf(w.m, m2), ref = mn == -INFINITY ? 0.f : mn;
+        const float f = fast_exp2(w.m - ref), f2 = fast_exp2(m2 - ref);
+        w.m = mn;
+        w.l = w.l * f + sl[wave][lane] * f2;
 #pragma unroll
-        for (int x = 0; x < W::NACC; ++x) w.o[0][x] = w.o[0][x] * f + so[wave][x][lane] * f2;
+        for (int x = 0; x < W::NACC; ++x) w.o[x] = w.o[x] * f + so[wave][x][lane] * f2;
       }
       __syncthreads();
     }
     const PagedTarget to = paged_target<kStreamRows, D, kShare>(a, s, blk, u0, u1, begins);
-    if (wave == 0 && valid) w.write(0, to, a, row, i, c);
+    if (wave == 0 && valid) w.write(to, a, row, i, c);
   });
 }
 
@@ -619,8 +621,8 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(8))) short s16x8;
 
-// The stream of tiles into LDS, 16 bytes a lane and load: wave w of 4 brings rows w, w + 1, .. of a quarter of a tile.  kSwzV: which
-// rows' pieces of V are permuted (see the kernels).
+// The stream of tiles into LDS, 16 bytes a lane and load: each of the 4 waves brings a quarter of a tile's rows, whose pages its
+// lanes look up a tile ahead.  The 16-byte pieces of a row are permuted in LDS by XOR with the row.
 template <typename T, int D>
 struct PagedTiles {
   static constexpr bool kBf16 = sizeof(T) == 2;
@@ -660,7 +662,9 @@ struct PagedTiles {
     const int page = min(max(entry, 0), a.pages.n_pages - 1);
     return (static_cast<uint32_t>(page) * a.pages.Hkv + g) * a.pages.page_size + at_row;
   }
-  // LDS serves 16 lanes of 16 bytes (32 of 8) at a time, from 64 banks: 256 bytes.  K: those lanes have 16 rows in a row; V: 4.
+  // LDS serves 16 lanes of 16 bytes (32 of 8) at a time, from 64 banks, 256 bytes: of K those lanes have the same piece of 16 rows
+  // in a row, of V (transposing reads) 64 bytes of 4 rows.  No conflicts so (45 % of the cycles that LDS was busy with K % 8 and
+  // 2 (V % 4)).
   static __device__ __forceinline__ int swizzle_k(int r) { return kRowBytes == 128 ? (r >> 1) & 7 : r & 15; }
   static __device__ __forceinline__ int swizzle_v(int r) { return !kBf16 ? 0 : D == 128 ? 4 * (r & 3) : 2 * (r & 2); }
   // the wave's rows of K or V of a tile on their way to `dst`; swizzle(row % 8): XORed to the index of a 16-byte piece
@@ -691,17 +695,23 @@ __device__ __forceinline__ f32x16 mma32(const u32x4& a, const u32x4& b, const f3
 }
 
 // Many queries: the tiles of 64 rows go through LDS, where the 4 waves of a workgroup share them, 32 (token, head) rows of a
-// group to a wave.  The next tile is on its way (straight into LDS, two buffers) while one is worked on.
+// group to a wave.  V of the next tile and K of the one behind it are on their way (straight into LDS, two buffers each) while
+// one is worked on, and the next tile's logits are computed among its exponentials.
 //
 // S^T = K Q^T in products of 32 x 32 x 16: a lane has one query (l % 32) and of 32 rows the 16 rows 8 (r / 4) + 4 h + r % 4,
 // h = l / 32.  Its weights are the B operand of O^T += V^T P^T as they are, since the order of the contraction is free: step s
 // of 32 rows takes 16 s + 4 h + {0..3, 8..11} from lane half h.  V^T comes from LDS by transposing reads: 16 lanes name 4 rows
 // x 4 pieces of 4 elements (lane i: row i / 4, piece i % 4) and get a column of 4 each; which elements of D make up the pieces
-// is free too, and is taken so that a lane ends with 8 neighbouring elements of its query's output.  16-byte pieces of a row
-// are permuted by XOR with the row in LDS (K: row % 8, V: 2 (row % 4)), which makes both kinds of reads free of conflicts.
+// is free too, and is taken so that a lane ends with 8 neighbouring elements of its query's output.
 //
 // Sums are taken against a reference that follows the maximum only when a tile exceeds it by 2^8 (any reference gives the
 // same result while nothing overflows), so that the outputs are rarely rescaled.
+//
+// Bound by the chip's power: a prompt of 16384 tokens, D = 128, 32 query and 8 KV heads, runs at 2160 us, 1020 TFLOP/s, with the
+// matrix cores busy half of the time at 1.75 GHz (a library's product of 8192 x 8192 matrices: 1314 TFLOP/s, 70 % at 1.67 GHz).
+// What raises the share of the time lowers the clock: without the logits ahead 45 % at 1.86 GHz, 2230 us.  Tried and no faster:
+// schedules given to the compiler, 8 waves of 32 rows to a workgroup, 4 waves of 64 (half the reads of LDS, one wave on a SIMD
+// and 36 % at 2.1 GHz: 2470 us; with D = 64 up to 10 % faster on prompts beyond 8000 tokens, 20 to 60 % slower on short ones).
 template <int D, bool kShare>
 __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
   using P = PagedTiles<bf16_t, D>;
@@ -883,7 +893,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
 template <int D, bool kShare>
 __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a) {
   using P = PagedTiles<float, D>;
-  using W = PagedWave<float, D, 1>;
+  using W = PagedWave<float, D>;
   constexpr int TK = P::TK, kRows = P::kRows;
   __shared__ __attribute__((aligned(16))) char s_k[2][P::kBytes], s_v[2][P::kBytes];
   const int lane = threadIdx.x & 63, wave = wave_index(), i = lane & 15, c = lane >> 4;
@@ -899,7 +909,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a)
     const int pos = valid ? blk.pos_of(a, r) : -1;
     W w;
     w.clear();
-    w.load_q(0, static_cast<const float*>(a.q) + static_cast<int64_t>(valid ? row : 0) * D, valid, c);
+    w.load_q(static_cast<const float*>(a.q) + static_cast<int64_t>(valid ? row : 0) * D, valid, c);
     P tiles{a, blk.table, g, wave, lane, 0, 0};
     const int u_end = min(u1, blk.kt.n);
     auto step = [&](int u, const char* __restrict kc, const char* __restrict vc, char* __restrict kn, char* __restrict vn) __attribute__((always_inline)) {
@@ -917,8 +927,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a)
           f32x4 sc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int kk = 0; kk < W::NK; ++kk)
-            mma_step<float>(sc, *reinterpret_cast<const u32x4*>(kc + (16 * t + i) * P::kRowBytes + (((4 * kk + c) ^ P::swizzle_k(i)) * 16)), w.qf[0][kk]);
-          w.template weigh<1>(0, &sc, t, base, from, to, pos, a, c);
+            mma_step<float>(sc, *reinterpret_cast<const u32x4*>(kc + (16 * t + i) * P::kRowBytes + (((4 * kk + c) ^ P::swizzle_k(i)) * 16)), w.qf[kk]);
+          w.template weigh<1>(&sc, t, base, from, to, pos, a, c);
 #pragma unroll
           for (int p = 0; p < W::NP; ++p) {
             u32x4 vf[4];
@@ -926,7 +936,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a)
             for (int y = 0; y < 4; ++y) vf[y] = *reinterpret_cast<const u32x4*>(vc + (16 * t + 4 * c + y) * P::kRowBytes + p * 256 + i * 16);
 #pragma unroll
             for (int x = 0; x < 4; ++x)
-              mma_step<float>(w.o[0][p * 4 + x], u32x4{vf[0][x], vf[1][x], vf[2][x], vf[3][x]}, __builtin_bit_cast(u32x4, sc));
+              mma_step<float>(w.o[p * 4 + x], u32x4{vf[0][x], vf[1][x], vf[2][x], vf[3][x]}, __builtin_bit_cast(u32x4, sc));
           }
         }
       }
@@ -946,8 +956,8 @@ __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a)
       if (u < u_end) step(u, s_k[0], s_v[0], s_k[1], s_v[1]);
     }
     const PagedTarget to = paged_target<kRows, D, kShare>(a, s, blk, u0, u1, begins);
-    w.l[0] = col4_sum(w.l[0]);
-    if (valid) w.write(0, to, a, row, r - blk.r0, c);
+    w.l = col4_sum(w.l);
+    if (valid) w.write(to, a, row, r - blk.r0, c);
   });
 }
 

@@ -398,8 +398,7 @@ def test_prompt_then_compression_then_decode():
     assert torch.equal(bufs.indices, plain.indices) and torch.equal(bufs.k_c, plain.k_c)
     # the compressed caches as pages of their capacity; the new token stands at position n of the text
     cap = bufs.cap
-    pc = cd.make_paged_params(dtype=dt, batch=nb, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_size=cap, n_pages=nb, max_pages=1, rot_dim=d)
-    grown = cd.PagedCache(pc, bufs.k_c.view(nb, hkv, cap, d), bufs.v_c.view(nb, hkv, cap, d), ints([[0], [1]]), bufs.cache_lens)
+    grown = bufs.paged(rot_dim=d)
     grown.reserve(nb, 1, cap)
     for t in range(3):
         q1, k1, v1 = (torch.randn((nb, h, d), generator=g, device=DEV) for h in (hq, hkv, hkv))
