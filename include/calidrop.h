@@ -513,7 +513,7 @@ int calidrop_paged_append(const calidrop_paged_params* p, const void* q, int64_t
  *   q             [total_q][Hq][D] dtype.    q_offsets  [batch+1] int32 or NULL.
  *   cache_lens    [batch] int32, rows of each cache including the tokens of this call; max_q_len >= the tokens and
  *                 max_cache_len >= the rows of every sequence (host copies; a longer cache is cut off there).
- *   out           out [total_q][Hq][D] dtype.    lse  out [total_q][Hq] fp32, natural log (the rows of the last tokens are
+ *   out           out [total_q][Hq][D] dtype; may be q itself.    lse  out [total_q][Hq] fp32, natural log (the rows of the last tokens are
  *                 the win_lse of calidrop_compress_with_lse).
  *   workspace     >= calidrop_paged_attend_workspace_bytes(p, total_q, max_q_len, max_cache_len) bytes, 256-byte aligned;
  *                 the size does not fall as any of the three grows.

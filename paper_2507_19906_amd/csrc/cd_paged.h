@@ -549,7 +549,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void paged_stream_kern
     const int r = blk.r0 + i;
     const bool valid = r < blk.R;
     const int t = valid ? divide(r, a.by_G) : 0;
-    const int row = static_cast<int>(blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);     // where valid; below 2^30
+    const int row = static_cast<int>(blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);     // where valid; below 2^29
     const int pos = valid ? blk.pos_of(a, r) : -1;
     W w;
     w.clear();
@@ -734,7 +734,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
     const int wr0 = blk.r0 + 32 * wave, r = wr0 + col;
     const bool valid = r < blk.R, any_rows = wr0 < blk.R;
     const int t = valid ? divide(r, a.by_G) : 0;
-    const int row = static_cast<int>(blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);       // where valid; below 2^30
+    const int row = static_cast<int>(blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);       // where valid; below 2^29
     const int pos = valid ? blk.pos_of(a, r) : -1;
     const int wave_min = blk.pos_of(a, wr0), wave_max = blk.pos_of(a, min(wr0 + 32, blk.R) - 1);
     u32x4 qf[NS];
@@ -905,7 +905,7 @@ __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a)
     const int wave_max = blk.pos_of(a, min(wr0 + 16, blk.R) - 1);
     const bool valid = r < blk.R;
     const int t0 = valid ? divide(r, a.by_G) : 0;
-    const int row = static_cast<int>(blk.q0 + t0) * a.Hq + g * a.G + (r - t0 * a.G);     // where valid; below 2^30
+    const int row = static_cast<int>(blk.q0 + t0) * a.Hq + g * a.G + (r - t0 * a.G);     // where valid; below 2^29
     const int pos = valid ? blk.pos_of(a, r) : -1;
     W w;
     w.clear();

@@ -69,7 +69,7 @@ cd::Pages pages_of(const calidrop_paged_params* p, const int32_t* table, int64_t
 // How an attention launch is cut up.  Up to 16 (token, head) rows stream the cache from memory to registers, more share tiles of
 // it in LDS.
 struct PagedPlan { bool stream; int rows, tile, least_shift; int64_t blocks, prefix, items, share, most_tiles; };      // share 0: a workgroup per block
-constexpr int kPagedStreamPlaces = 768, kPagedTilePlaces = 512;        // workgroups the chip holds at a time
+constexpr int kPagedStreamPlaces = 768, kPagedTilePlaces = 512;        // workgroups the chip holds at a time (bf16, D = 128)
 constexpr int64_t kPagedMostItems = 4096;                              // every workgroup adds up their tiles
 
 // Most tiles that a block can need (cd::KeyTiles): under a window, the rows of the window and of the sinks can begin and end
@@ -172,12 +172,12 @@ int check_attend_sizes(const calidrop_paged_params* p, int64_t total_q, int32_t 
   if (total_q < 0 || max_q_len < 1 || max_cache_len < 0)
     return fail(CALIDROP_ESHAPE, "total_q >= 0, max_q_len >= 1 and max_cache_len >= 0 expected (got %lld, %d, %d)",
                 static_cast<long long>(total_q), max_q_len, max_cache_len);
-  if (total_q > (int64_t{1} << 30) / p->n_q_heads)
-    return fail(CALIDROP_EUNSUPPORTED, "total_q * n_q_heads exceeds 2^30");
+  if (total_q > (int64_t{1} << 29) / p->n_q_heads)
+    return fail(CALIDROP_EUNSUPPORTED, "total_q * n_q_heads exceeds 2^29");
   const int64_t G = p->n_q_heads / p->n_kv_heads;
   if (max_q_len > (1 << 26) / G) return fail(CALIDROP_EUNSUPPORTED, "max_q_len * (n_q_heads / n_kv_heads) exceeds 2^26");
-  if ((max_q_len * G + 63) / 64 * p->n_kv_heads * p->batch >= 1 << 24)          // workgroups of 256 threads on one grid axis
-    return fail(CALIDROP_EUNSUPPORTED, "batch * max_q_len * n_q_heads exceeds 2^30");
+  if ((max_q_len * G + 63) / 64 * p->n_kv_heads * p->batch > 1 << 23)           // with a prefix's, below 2^24 workgroups of 256 threads
+    return fail(CALIDROP_EUNSUPPORTED, "batch * max_q_len * n_q_heads exceeds 2^29");
   if (max_cache_len > paged_capacity(p))
     return fail(CALIDROP_ESHAPE, "max_cache_len %d exceeds the max_pages * page_size = %lld rows of a table", max_cache_len,
                 static_cast<long long>(paged_capacity(p)));

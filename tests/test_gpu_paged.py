@@ -253,6 +253,22 @@ def test_both_forms_of_a_call(dtype, d):
     assert launches([50, 3], [1, 1], one=True, prefix=300) == 2
 
 
+@pytest.mark.parametrize("dtype,d", TYPES)
+def test_empty_caches(dtype, d):
+    Setup([0, 0, 0], [1, 1, 1], 8, 2, d, dtype, 16, one=True, seed=19).run().check()
+    Setup([0, 0, 0], [2, 40, 0], 8, 2, d, dtype, 16, seed=19).run().check()
+    Setup([0, 0, 0], [1, 1, 1], 8, 2, d, dtype, 16, prefix=45, one=True, seed=19).run().check()
+    Setup([0, 0, 0], [2, 40, 0], 8, 2, d, dtype, 16, prefix=45, seed=19).run().check()
+
+
+@pytest.mark.parametrize("lens,nq,prefix", [([70, 33], [1, 1], 0), ([4000, 33], [3, 2], 0), ([200, 130], [200, 90], 0), ([6000], [70], 0),
+                                            ([30, 70], [20, 1], 500)])
+def test_results_in_the_place_of_the_queries(lens, nq, prefix):
+    s = Setup(lens, nq, 8, 2, 128, "bf16", 16, prefix=prefix, seed=20)
+    s.out = s.qd
+    s.run().check()
+
+
 def test_lengths_that_cannot_be():
     # below zero: no rows; above what the host was told: cut off there, the queries ending at the cut
     s = Setup([40, 70, 90], [2, 1, 3], 8, 2, 64, "bf16", 16, seed=17)
