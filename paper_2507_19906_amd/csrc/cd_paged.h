@@ -276,14 +276,14 @@ struct PagedBlock {
 };
 
 // The tiles lo .. hi-1 of all blocks of KV head g are workgroup w's; they begin in block `item`, whose first tile is `start`.
-struct PagedShare { int lo, hi, start, total, each, more, item, g, w, W; };      // tiles of a launch: below 2^31
+struct PagedShare { int lo, hi, start, item, g, w; };      // tiles of a launch: below 2^31
 
 template <int kRows, int TK, bool kShare>
 __device__ __forceinline__ PagedShare paged_share(const PagedAttendArgs& a, uint32_t* scratch) {
   PagedShare s;
   const int Hkv = a.pages.Hkv, x = blockIdx.x;
   PagedBlock<kRows, TK> blk;
-  s.lo = s.hi = s.start = s.w = s.W = s.each = s.more = 0;
+  s.lo = s.hi = s.start = s.item = s.w = 0;
   if constexpr (!kShare) {
     // blocks of a (sequence, KV head) behind one L2 and the heads of every sequence spread over the XCDs, which workgroups go
     // to in turn; the longest blocks of a prompt first
@@ -303,9 +303,10 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttendArgs& a, uint
   // the tiles of all blocks added up: a thread has up to (items + 255) / 256 blocks in a row
   const int tid = threadIdx.x, per = (a.items + 255) / 256, i0 = tid * per, i1 = min(i0 + per, a.items);
   uint32_t mine = 0, before = 0;
+  int total;
   if (a.items == 1) {
     blk.init(a, 0);
-    s.total = blk.weight();
+    total = blk.weight();
   } else {
     for (int it = i0; it < i1; ++it) { blk.init(a, it); mine += blk.weight(); }
     const uint32_t upto = wave_inclusive_scan(mine);
@@ -313,11 +314,10 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttendArgs& a, uint
     __syncthreads();
     const uint32_t t0 = scratch[0], t1 = scratch[1], t2 = scratch[2], t3 = scratch[3];
     before = upto - mine + (tid >= 64 ? t0 : 0) + (tid >= 128 ? t1 : 0) + (tid >= 192 ? t2 : 0);
-    s.total = __builtin_amdgcn_readfirstlane(t0 + t1 + t2 + t3);
+    total = __builtin_amdgcn_readfirstlane(t0 + t1 + t2 + t3);
   }
-  s.W = min(max(s.total >> a.least_shift, 1), a.share);
-  s.item = 0;
-  if (s.W == a.share && 8 % Hkv == 0 && a.share % (8 / Hkv) == 0) {      // neighbouring shares behind one L2
+  const int W = min(max(total >> a.least_shift, 1), a.share);
+  if (W == a.share && 8 % Hkv == 0 && a.share % (8 / Hkv) == 0) {      // neighbouring shares behind one L2
     const int xcd = x % 8;
     s.g = xcd % Hkv;
     s.w = xcd / Hkv * (a.share / (8 / Hkv)) + x / 8;
@@ -325,11 +325,10 @@ __device__ __forceinline__ PagedShare paged_share(const PagedAttendArgs& a, uint
     s.w = divide(x, a.by_Hkv);
     s.g = x - s.w * Hkv;
   }
-  if (s.w >= s.W) return s;
-  s.each = static_cast<uint32_t>(s.total) / static_cast<uint32_t>(s.W);
-  s.more = s.total - s.each * s.W;                     // the first of them have one tile more
-  s.lo = s.each * s.w + min(s.w, s.more);
-  s.hi = s.lo + s.each + (s.w < s.more ? 1 : 0);
+  if (s.w >= W) return s;
+  const int each = static_cast<uint32_t>(total) / static_cast<uint32_t>(W), more = total - each * W;      // the first `more` have one tile more
+  s.lo = each * s.w + min(s.w, more);
+  s.hi = s.lo + each + (s.w < more ? 1 : 0);
   if (a.items > 1) {
     if (before <= static_cast<uint32_t>(s.lo) && static_cast<uint32_t>(s.lo) < before + mine) {
       uint32_t at = before;
@@ -363,11 +362,10 @@ __device__ __forceinline__ PagedTarget paged_target(const PagedAttendArgs& a, co
   const int64_t side = blk.prefix ? a.total_q * a.Hq : 0;
   const PagedTarget whole{a.prefix_items == 0, true, a.whole_o + side * D, a.whole_ml + side};
   if constexpr (!kShare) return whole;
-  if (s.g == 0 && u0 == 0 && threadIdx.x == 0) {
-    // the workgroup that the block's last tile is in the share of
-    const uint32_t x = s.start + blk.weight() - 1, longer = s.more * (s.each + 1);
-    const uint32_t last = x < longer ? x / (s.each + 1) : s.more + (x - longer) / s.each;
-    a.cut[s.item] = int4{s.w, static_cast<int>(last), begins ? 0 : 1, 0};
+  if (s.g == 0 && threadIdx.x == 0) {                  // the heads are cut alike
+    int* cut = reinterpret_cast<int*>(a.cut + s.item);
+    if (u0 == 0) { cut[0] = s.w; cut[2] = begins ? 0 : 1; }
+    if (u1 == blk.kt.n) cut[1] = s.w;
   }
   if (u0 == 0 && u1 == blk.kt.n) return whole;
   const int64_t slot = (static_cast<int64_t>(s.g) * a.share + s.w) * 2 + (begins ? 0 : 1);
