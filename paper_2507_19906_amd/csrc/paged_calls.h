@@ -95,7 +95,7 @@ PagedPlan paged_blocks(const calidrop_paged_params* p, int64_t total_q, int64_t 
   plan.items = plan.prefix + p->batch * plan.blocks;
   plan.most_tiles = most_tiles(p, q_len, max_len, plan.rows, plan.tile);
   const int64_t most = std::max<int64_t>(1, (plan.stream ? kPagedStreamPlaces : kPagedTilePlaces) / p->n_kv_heads);
-  const int setup = plan.stream ? cd::PagedBlock<16, 32>::kSetup : cd::PagedBlock<128, 64>::kSetup;
+  const int setup = plan.stream ? cd::PagedBlock<16, 32>::kSetup : fp32 ? cd::PagedBlock<64, 32>::kSetup : cd::PagedBlock<128, 64>::kSetup;
   const int64_t tiles = std::min(plan.prefix, kPagedMostItems) * ((shared_len + plan.tile - 1) / plan.tile + setup) +
                         std::min(plan.items - plan.prefix, kPagedMostItems) * (plan.most_tiles + setup);
   plan.share = std::max<int64_t>(1, std::min(most, tiles >> plan.least_shift));
