@@ -14,6 +14,9 @@
  *                        calidrop_decode flagged: refresh the calibration state from KV_evict
  *                        with the current query and calibrate the step's output.
  *
+ * Around them: growth of the compressed cache, other eviction strategies, the evicted rows in a movable form, and a cache in
+ * pages with the attention that reads it.
+ *
  * Conventions shared by every entry point
  *   - All data pointers are DEVICE pointers owned by the caller (for example a torch
  *     tensor's data_ptr(); the one exception is stated at calidrop_recalibrate_packed); they
@@ -187,7 +190,7 @@ int calidrop_compress(const calidrop_params* p, const void* q_win, const void* k
  *
  * The softmax of step 1 needs, for every window query i of every query head, the log-sum-exp of
  * its logits over the keys it may attend to (positions 0..P+i).  The prefill attention that
- * produced the prompt's outputs (Alg. 1 steps 1-2, outside this library) has that number for
+ * produced the prompt's outputs (Alg. 1 steps 1-2; calidrop_paged_attend, say) has that number for
  * every query row as the by-product of its own softmax; passing it in saves the pass over K that
  * calidrop_compress spends on it (K is then read once, for the votes, instead of twice).
  *
