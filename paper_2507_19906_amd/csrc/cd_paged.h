@@ -550,9 +550,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void paged_stream_kern
     const int t = valid ? divide(r, a.by_G) : 0;
     const int row = static_cast<int>(blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);     // where valid; below 2^29
     const int pos = valid ? blk.pos_of(a, r) : -1;
-    W w;
-    w.clear();
-    w.load_q(static_cast<const T*>(a.q) + static_cast<int64_t>(valid ? row : 0) * D, valid, c);
     auto row_of = [&](int u) -> uint32_t {                   // of row lane % 32 of the tile
       int base, from, to;
       blk.kt.tile(u, base, from, to);
@@ -561,6 +558,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void paged_stream_kern
     const int u_end = min(u1, blk.kt.n);
     int u = u0 + wave;
     uint32_t rid = u < u_end ? row_of(u) : 0;
+    // behind the look-up: loads return in the order of their requests
+    W w;
+    w.clear();
+    w.load_q(static_cast<const T*>(a.q) + static_cast<int64_t>(valid ? row : 0) * D, valid, c);
     while (u < u_end) {
       u32x4 kf[2][W::NK];
       typename W::VPiece vf[8][W::NP];
@@ -712,7 +713,7 @@ __device__ __forceinline__ f32x16 mma32(const u32x4& a, const u32x4& b, const f3
 // schedules given to the compiler, 8 waves of 32 rows to a workgroup, 4 waves of 64 (half the reads of LDS, one wave on a SIMD
 // and 36 % at 2.1 GHz: 2470 us; with D = 64 up to 10 % faster on prompts beyond 8000 tokens, 20 to 60 % slower on short ones).
 template <int D, bool kShare>
-__global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
+__global__ __launch_bounds__(256, D == 64 && !kShare ? 3 : 2) void paged_tile_kernel(PagedAttendArgs a) {
   using P = PagedTiles<bf16_t, D>;
   constexpr int TK = P::TK, kRows = P::kRows, NS = D / 16, ND = D / 32;
   __shared__ __attribute__((aligned(16))) char s_k[2][P::kBytes], s_v[2][P::kBytes];
@@ -736,6 +737,16 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
     const int row = static_cast<int>(blk.q0 + t) * a.Hq + g * a.G + (r - t * a.G);       // where valid; below 2^29
     const int pos = valid ? blk.pos_of(a, r) : -1;
     const int wave_min = blk.pos_of(a, wr0), wave_max = blk.pos_of(a, min(wr0 + 32, blk.R) - 1);
+    P tiles{a, blk.table, g, wave, lane, 0, 0};
+    const int u_end = min(u1, blk.kt.n);
+    uint32_t first = 0, rid = 0;                         // this wave's rows of the tile that K was last requested of
+    if (u0 < u_end) {
+      tiles.look_up(blk.kt, u0, min(u0 + 1, u_end - 1), min(u0 + 2, u_end - 1), first, rid);
+      tiles.issue_k(first, s_k[0]);
+      tiles.issue_v(first, s_v[0]);
+      if (u0 + 1 < u_end) tiles.issue_k(rid, s_k[1]);
+    }
+    // behind the look-up: loads return in the order of their requests
     u32x4 qf[NS];
 #pragma unroll
     for (int st = 0; st < NS; ++st) qf[st] = valid ? ld16(static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(row) * D + st * 16 + h * 8) : zero16();
@@ -745,8 +756,6 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
     float ref = -INFINITY, l = 0.f;                      // reference (unscaled logits), this lane's share of the sum
-    P tiles{a, blk.table, g, wave, lane, 0, 0};
-    const int u_end = min(u1, blk.kt.n);
     auto logits = [&](const char* __restrict kc, f32x16 (&sc)[2]) __attribute__((always_inline)) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -760,7 +769,6 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
           sc[kb] = mma32(kf, qf[st], sc[kb]);
         }
     };
-    uint32_t rid = 0;                                    // this wave's rows of the tile that K was last requested of
     // tile u, whose logits are sc: the next tile's logits are computed (from kc) among the exponentials of this one's
     auto step = [&](int u, f32x16 (&sc)[2], f32x16 (&nx)[2], const char* __restrict kc, const char* __restrict vc, char* __restrict kn,
                     char* __restrict vn) __attribute__((always_inline)) {
@@ -840,11 +848,6 @@ __global__ __launch_bounds__(256, 2) void paged_tile_kernel(PagedAttendArgs a) {
     };
     if (u0 < u_end) {
       f32x16 sa[2], sb[2];
-      uint32_t first = 0;
-      tiles.look_up(blk.kt, u0, min(u0 + 1, u_end - 1), min(u0 + 2, u_end - 1), first, rid);
-      tiles.issue_k(first, s_k[0]);
-      tiles.issue_v(first, s_v[0]);
-      if (u0 + 1 < u_end) tiles.issue_k(rid, s_k[1]);
       tiles.landed();
       logits(s_k[0], sa);
       tiles.landed();                                    // the first step overwrites what was read here
@@ -906,11 +909,17 @@ __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a)
     const int t0 = valid ? divide(r, a.by_G) : 0;
     const int row = static_cast<int>(blk.q0 + t0) * a.Hq + g * a.G + (r - t0 * a.G);     // where valid; below 2^29
     const int pos = valid ? blk.pos_of(a, r) : -1;
+    P tiles{a, blk.table, g, wave, lane, 0, 0};
+    const int u_end = min(u1, blk.kt.n);
+    if (u0 < u_end) {
+      uint32_t rid, none;
+      tiles.look_up(blk.kt, u0, u0, min(u0 + 1, u_end - 1), rid, none);
+      tiles.issue_k(rid, s_k[0]);
+      tiles.issue_v(rid, s_v[0]);
+    }
     W w;
     w.clear();
     w.load_q(static_cast<const float*>(a.q) + static_cast<int64_t>(valid ? row : 0) * D, valid, c);
-    P tiles{a, blk.table, g, wave, lane, 0, 0};
-    const int u_end = min(u1, blk.kt.n);
     auto step = [&](int u, const char* __restrict kc, const char* __restrict vc, char* __restrict kn, char* __restrict vn) __attribute__((always_inline)) {
       if (u + 1 < u_end) {
         const uint32_t rid = tiles.row_number();
@@ -942,10 +951,6 @@ __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a)
       tiles.landed();
     };
     if (u0 < u_end) {
-      uint32_t rid, none;
-      tiles.look_up(blk.kt, u0, u0, min(u0 + 1, u_end - 1), rid, none);
-      tiles.issue_k(rid, s_k[0]);
-      tiles.issue_v(rid, s_v[0]);
       tiles.landed();
       int u = u0;
       for (; u + 1 < u_end; u += 2) {
