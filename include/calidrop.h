@@ -449,7 +449,8 @@ int calidrop_recalibrate_packed(const calidrop_params* p, const void* q_t, const
  * page_table[b][r / page_size].  Entries behind the last row a call needs are not read, nor are those of rows that no query
  * of a call sees under a window.  The tables are device memory, so the host cannot check them: rows on an entry outside
  * [0, n_pages) are not written by calidrop_paged_append and read as some existing page by the attention calls - memory safe,
- * result meaningless.  K and V rows that a query of a call sees must be finite; what other rows hold does not matter.
+ * result meaningless.  K and V rows that a query of a call sees must be finite (what is not may reach other queries of the
+ * call); what other rows hold does not matter.
  *
  * Tokens of a call are packed: those of sequence b are offsets[b] .. offsets[b+1]-1 (any number, none included), where NULL
  * offsets mean one token per sequence (then the total must be batch).  For tokens that no sequence owns (behind the last one)

@@ -1009,7 +1009,7 @@ int h2o_impl(const calidrop_params* p, int n_local, const void* q_full, const vo
 extern "C" {
 
 const char* calidrop_last_error(void) { return g_err; }
-int calidrop_version(void) { return 200; }
+int calidrop_version(void) { return 300; }
 
 size_t calidrop_compress_workspace_bytes(const calidrop_params* p_in, int64_t total_tokens, int32_t max_seq_len) {
   calidrop_params pp; const calidrop_params* p = &pp;

@@ -110,7 +110,7 @@ PagedPlan paged_blocks(const calidrop_paged_params* p, int64_t total_q, int64_t 
 //   tiles, bf16, D = 128: 64 queries at 1000 rows 29 / 24, at 16000 359 / 44; 512 queries of a prompt 17.6 / 32.5, at 8512 rows
 //   193 / 102; 4 sequences of those 289 / 320; 2 prompts of 2048 87 / 170.
 // The host does not know how the lengths of several sequences differ.  The shared form does not care (4 chunks of 300 to 512
-// queries behind 8000 to 32000 rows 813 / 427, 64 queries of 1000 to 16000 rows 541 / 348), so it may cost `ragged` times the
+// queries behind 8000 to 32000 rows 813 / 450, 64 queries of 1000 to 16000 rows 541 / 348), so it may cost `ragged` times the
 // other there.  Calls of many blocks level themselves out.
 struct PagedCost { float stream_tile, single, pair, pair_shared; };      // us a tile, alone on a compute unit and in pairs
 PagedPlan plan_paged(const calidrop_paged_params* p, int64_t total_q, int64_t q_len, int64_t max_len, int64_t shared_len) {

@@ -477,6 +477,28 @@ def test_a_captured_step_replays_to_the_eager_results():
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("lens,nq,prefix", [([5000, 300, 2000], [1, 1, 1], 0), ([6000, 900], [40, 30], 0), ([300, 40], [3, 30], 2000)])
+def test_a_captured_call_follows_the_lengths(lens, nq, prefix):
+    # the lengths are read on the device: replays after they have changed, with eager work between, give what eager calls give
+    s = Setup(lens, nq, 8, 2, 128, "bf16", 16, prefix=prefix, seed=37)
+    s.cache.k_pages.nan_to_num_(0.5), s.cache.v_pages.nan_to_num_(0.5)         # shorter caches end elsewhere
+    s.run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        s.run()
+    for cut in ([0] * 3, [10, 0, 1], [900, 35, 1999], [0, 7, 3], [1, 1, 1]):
+        s.cache.cache_lens.copy_(ints([n - c for n, c in zip(lens, cut)]))
+        s.run()
+        torch.cuda.synchronize()
+        eager = s.out.clone(), s.lse.clone()
+        s.out.fill_(77), s.lse.fill_(77)
+        s.cache.workspace.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(s.out, eager[0]) and torch.equal(s.lse, eager[1])
+
+
 def test_results_do_not_depend_on_the_run():
     s = Setup([3000, 200, 900], [2, 1, 4], 8, 2, 128, "bf16", 16, prefix=700, seed=32).run()
     torch.cuda.synchronize()
