@@ -203,6 +203,9 @@ int attend_impl(const calidrop_paged_params* p, cd::PagedAttendArgs& a, char* ws
   a.part_ml = reinterpret_cast<float2*>(ws + R.part_ml); a.part_o = reinterpret_cast<float*>(ws + R.part_o);
   a.whole_ml = reinterpret_cast<float2*>(ws + R.whole_ml); a.whole_o = reinterpret_cast<float*>(ws + R.whole_o);
   void (*kernel)(cd::PagedAttendArgs);
+  // Behind a prefix the few queries of a sequence's own rows go through the tile kernel too, a wave of four at work: streamed
+  // without LDS in the same launch, as the streaming kernel does alone, they were no faster (64 queries, 32768 + 0 to 512 rows
+  // 72 for 67 us; 256 queries, 8000 + 10 to 300 rows 86 both), since two waves on a SIMD hide less than loads two tiles ahead.
   if (plan.stream) kernel = plan.share ? cd::paged_stream_kernel<T, D, true> : cd::paged_stream_kernel<T, D, false>;
   else if constexpr (sizeof(T) == 2) kernel = plan.share ? cd::paged_tile_kernel<D, true> : cd::paged_tile_kernel<D, false>;
   else kernel = plan.share ? cd::paged_tile32_kernel<D, true> : cd::paged_tile32_kernel<D, false>;
