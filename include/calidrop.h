@@ -491,7 +491,8 @@ typedef struct {
  * Arguments
  *   q, k, v       [total_new][Hq or Hkv][D] dtype, consecutive tokens q_stride / k_stride / v_stride elements apart (parts of
  *                 one projection's output, say): a multiple of 16 bytes, at least heads * D.  q may be NULL (with q_out).
- *   new_offsets   [batch+1] int32 or NULL; max_new >= the tokens of every sequence (host copy; sizes the grid).
+ *   new_offsets   [batch+1] int32 or NULL; max_new >= the tokens of every sequence (host copy; sizes the grid): of a sequence
+ *                 with more, the first max_new are its tokens.
  *   positions     [total_new] int32, or NULL: the row in the cache.
  *   rot_table     fp32 [n_positions][rot_dim]: the cosines of position p's rot_dim / 2 angles, then their sines.  Positions
  *                 outside [0, n_positions) take the nearest entry.  NULL when rot_dim = 0.
@@ -516,7 +517,8 @@ int calidrop_paged_append(const calidrop_paged_params* p, const void* q, int64_t
  *
  *   q             [total_q][Hq][D] dtype.    q_offsets  [batch+1] int32 or NULL.
  *   cache_lens    [batch] int32, rows of each cache including the tokens of this call; max_q_len >= the tokens and
- *                 max_cache_len >= the rows of every sequence (host copies; a longer cache is cut off there).
+ *                 max_cache_len >= the rows of every sequence (host copies; a longer cache is cut off there, and of a sequence with
+ *                 more tokens the first max_q_len are taken for its newest ones).
  *   out           out [total_q][Hq][D] dtype; may be q itself.    lse  out [total_q][Hq] fp32, natural log (the rows of the last tokens are
  *                 the win_lse of calidrop_compress_with_lse).
  *   workspace     >= calidrop_paged_attend_workspace_bytes(p, total_q, max_q_len, max_cache_len) bytes, 256-byte aligned;

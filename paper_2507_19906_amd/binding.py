@@ -600,12 +600,19 @@ class PagedCache:
         if self.workspace is None or self.workspace.nbytes < n:
             self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
 
-    def append(self, k, v, q=None, q_out=None, new_offsets=None, max_new: int = 1, positions=None, rot_table=None, new_lens=None,
-               stream=None) -> None:
+    @staticmethod
+    def _most(given: Optional[int], offsets, total: int) -> int:
+        """Most tokens of a sequence: as given, or what holds for any offsets.  (The kernels take no more than that of each.)"""
+        return given if given is not None else 1 if offsets is None else max(total, 1)
+
+    def append(self, k, v, q=None, q_out=None, new_offsets=None, max_new: Optional[int] = None, positions=None, rot_table=None,
+               new_lens=None, stream=None) -> None:
         """k, v [total][Hkv][D] become the next rows of the sequences, rotated on the way; q [total][Hq][D] goes rotated to q_out.
-        new_lens None: cache_lens grows in place."""
+        max_new: no fewer than the tokens of any sequence (of more, the first max_new are taken); None with offsets: total, at the
+        price of more workgroups.  new_lens None: cache_lens grows in place."""
         fits = self._fits
         total, hkv = k.shape[0], self.n_kv_heads
+        max_new = self._most(max_new, new_offsets, total)
         ks, vs, qs = self._heads(k, "k", total, hkv), self._heads(v, "v", total, hkv), 0
         if (q is None) != (q_out is None):
             raise ValueError("q and q_out go together")
@@ -633,6 +640,7 @@ class PagedCache:
         at_q, at_out = fits(q, "q", self.dtype, shape), fits(out, "out", self.dtype, shape)
         at_lse = fits(lse, "lse", torch.float32, (total, hq))
         at_offsets = None if q_offsets is None else fits(q_offsets, "q_offsets", torch.int32, (self.batch + 1,))
+        max_q_len = self._most(max_q_len, q_offsets, total)
         if max_cache_len is None:
             max_cache_len = self.capacity
         ws = self.workspace
@@ -648,11 +656,14 @@ class PagedCache:
                                                     at_out, at_lse, at_ws, n_ws, st)
         _check(status)
 
-    def attend(self, q, out, lse, q_offsets=None, max_q_len: int = 1, max_cache_len: Optional[int] = None, stream=None) -> None:
-        """Attention of the newest tokens, q [total][Hq][D], over the cache, into out and lse [total][Hq]."""
+    def attend(self, q, out, lse, q_offsets=None, max_q_len: Optional[int] = None, max_cache_len: Optional[int] = None,
+               stream=None) -> None:
+        """Attention of the newest tokens, q [total][Hq][D], over the cache, into out and lse [total][Hq].  max_q_len and
+        max_cache_len: no fewer than the tokens and the rows of any sequence.  None: total with offsets and the capacity of the
+        tables, which are right for any call; closer ones let the library cut the call up better and need less workspace."""
         self._attend(None, q, out, lse, q_offsets, max_q_len, max_cache_len, stream)
 
-    def attend_shared(self, q, out, lse, shared_table, shared_len: int, q_offsets=None, max_q_len: int = 1,
+    def attend_shared(self, q, out, lse, shared_table, shared_len: int, q_offsets=None, max_q_len: Optional[int] = None,
                       max_cache_len: Optional[int] = None, stream=None) -> None:
         """The same behind a prefix of shared_len rows in the pages shared_table."""
         at = self._fits(shared_table, "shared_table", torch.int32, (-(-shared_len // self.page_size),))

@@ -291,6 +291,16 @@ def test_offsets_that_cannot_be():
     assert torch.equal(got[:1], s.out[:1])
 
 
+@pytest.mark.parametrize("lens,nq,prefix", [([70, 33, 9], [1, 3, 2], 0), ([300, 200, 64], [130, 0, 7], 0), ([4000, 33], [3, 2], 0),
+                                            ([30, 70, 12], [20, 1, 12], 333)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_offsets_without_a_bound(dtype, lens, nq, prefix):
+    s = Setup(lens, nq, 8, 2, 64, dtype, 16, prefix=prefix, seed=38, spare_tokens=2)
+    del s.most["max_q_len"]
+    s.cache.reserve(s.total, s.total, max(lens), prefix)
+    s.run().check()
+
+
 # ---- append -------------------------------------------------------------------------------------------------------------------
 
 def append_case(dtype, d, hq, hkv, page, lens, nq, rot, pairs, seed, max_pages=None, one=False, positions=True, with_q=True, in_place=False, bad=False):
@@ -379,6 +389,31 @@ def test_append_of_nothing():
     assert new_lens.tolist() == [3, 4]
     s.cache.append(none, none, new_offsets=ints([0, 0, 0]), max_new=50)
     assert s.cache.cache_lens.tolist() == [3, 4]
+
+
+@pytest.mark.parametrize("bound,offsets,rows", [
+    (None, [0, 3, 3, 12], [(0, 3), (3, 0), (3, 9)]),                    # no bound given: every token
+    (2, [0, 3, 3, 12], [(0, 2), (3, 0), (3, 2)]),                       # below the tokens of a sequence: its first ones
+    (12, [0, 2, 1, 1 << 30], [(0, 2), (2, 0), (1, 11)]),                # falling, and beyond the tokens: what is in range
+    (12, [-9, 2, -5, 4], [(0, 2), (2, 0), (0, 4)])])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_append_bounds_and_offsets(bound, offsets, rows, in_place):
+    nb, hq, hkv, d, page, lens = 3, 4, 2, 64, 16, [5, 0, 16]
+    g = torch.Generator(device=DEV).manual_seed(39)
+    k, v, q = (torch.randn((12, h, d), generator=g, device=DEV) for h in (hkv, hkv, hq))
+    p = cd.make_paged_params(dtype="fp32", batch=nb, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, page_size=page, n_pages=9, max_pages=3)
+    c = cd.PagedCache(p, torch.zeros((9, hkv, page, d), device=DEV), torch.zeros((9, hkv, page, d), device=DEV),
+                      torch.arange(9, dtype=torch.int32, device=DEV).view(3, 3), ints(lens))
+    q_out, new_lens = torch.full_like(q, 77.0), None if in_place else ints([0] * nb)
+    c.append(k, v, q=q, q_out=q_out, new_offsets=ints(offsets), max_new=bound, new_lens=new_lens)
+    want_k, want_v, want_q = torch.zeros_like(c.k_pages), torch.zeros_like(c.v_pages), torch.full_like(q, 77.0)
+    for b, (first, n) in enumerate(rows):
+        want_q[first:first + n] = q[first:first + n]
+        for t in range(n):
+            r = lens[b] + t
+            want_k[3 * b + r // page, :, r % page], want_v[3 * b + r // page, :, r % page] = k[first + t], v[first + t]
+    assert torch.equal(c.k_pages, want_k) and torch.equal(c.v_pages, want_v) and torch.equal(q_out, want_q)
+    assert (c.cache_lens if in_place else new_lens).tolist() == [n + r[1] for n, r in zip(lens, rows)]
 
 
 # ---- together ---------------------------------------------------------------------------------------------------------------------

@@ -239,3 +239,37 @@ def test_calls_on_a_cache_off_the_current_gpu_are_refused():
     q = torch.zeros((2, 4, 64), dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="current device"):
         c.attend(q, q.clone(), torch.zeros((2, 4)))
+
+
+class Recorder:
+    """In the library's place: keeps the arguments of each call by name."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append((name, args)) or cd.OK
+
+
+def recorded_cache(monkeypatch, **kw):
+    """A cache whose calls end at the recorder: whatever they are given stays on the host."""
+    c, lib = cpu_cache(**kw), Recorder()
+    monkeypatch.setattr(cd, "_lib", lib)
+    monkeypatch.setattr(c, "_on_device", lambda stream: stream)
+    return c, lib
+
+
+def test_without_a_bound_the_tokens_of_a_sequence_are_at_most_all():
+    bf = torch.bfloat16
+    for total, offsets, want in [(7, torch.tensor([0, 6, 7], dtype=torch.int32), 7), (0, torch.zeros(3, dtype=torch.int32), 1), (2, None, 1)]:
+        with pytest.MonkeyPatch.context() as mp:
+            c, lib = recorded_cache(mp)
+            q, k, lse = torch.zeros((total, 4, 64), dtype=bf), torch.zeros((total, 2, 64), dtype=bf), torch.zeros((total, 4))
+            prefix = torch.zeros(2, dtype=torch.int32)
+            c.append(k, k, new_offsets=offsets, rot_table=torch.zeros((9, 32)))
+            c.attend(q, q.clone(), lse, q_offsets=offsets)
+            c.attend_shared(q, q.clone(), lse, prefix, 20, q_offsets=offsets)
+            c.append(k, k, new_offsets=offsets, max_new=5, rot_table=torch.zeros((9, 32)))
+            c.attend(q, q.clone(), lse, q_offsets=offsets, max_q_len=5)
+        # max_new is argument 9 of append, max_q_len argument 4 of both others
+        assert [args[9 if name.endswith("append") else 4] for name, args in lib.calls] == [want, want, want, 5, 5]
