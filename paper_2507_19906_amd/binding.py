@@ -212,6 +212,10 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream or None
 
 
+def _stream_object(raw: Optional[int], device):
+    return torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
+
+
 def calidrop_compress_workspace_bytes(p: Params, total_tokens: int, max_seq_len: int) -> int:
     n = lib().calidrop_compress_workspace_bytes(ctypes.byref(p), total_tokens, max_seq_len)
     if n == 0:
@@ -549,7 +553,8 @@ class PagedCache:
     (shapes, types, layouts, the device) and refuses what does not fit with ValueError.
 
     k_pages, v_pages [n_pages][Hkv][page_size][D]; page_table [batch][max_pages] int32; cache_lens [batch] int32.  The tensors
-    stay the caller's: new pages are handed out by writing page_table.  `p` is copied: later changes of it are not seen."""
+    stay the caller's: new pages are handed out by writing page_table.  `p` is copied: later changes of it are not seen.
+    `workspace` may be replaced while calls run on any stream: its memory is not handed out again before they have ended."""
 
     def __init__(self, p: PagedParams, k_pages, v_pages, page_table, cache_lens):
         self.p = PagedParams.from_buffer_copy(p)
@@ -566,6 +571,23 @@ class PagedCache:
         self._fits(cache_lens, "cache_lens", torch.int32, (p.batch,))
         self.k_pages, self.v_pages, self.page_table, self.cache_lens = k_pages, v_pages, page_table, cache_lens
         self.workspace = None
+
+    @property
+    def workspace(self):
+        """What reserve() allocated, or a tensor of the caller's."""
+        return self._workspace
+
+    @workspace.setter
+    def workspace(self, t):
+        if t is not None and (t.device != self.device or not t.is_contiguous()):
+            raise ValueError(f"workspace: a contiguous tensor on {self.device} expected, not one on {t.device} with strides {list(t.stride())}")
+        self._workspace, self._workspace_streams = t, set()
+
+    def _hold(self, ws, st) -> None:
+        # the allocator takes memory for free, once nobody holds it, as soon as the stream it was allocated on gets there, unless
+        # it is told which others use it
+        ws.record_stream(_stream_object(st, self.device))
+        self._workspace_streams.add(st)
 
     # The checks of a call take as long as its launch, so they ask for little: a device as its number, parameters as plain
     # attributes (append of single tokens 9.3 us a call with a tensor's device object and the parameters' fields, 7.0 so).
@@ -593,11 +615,12 @@ class PagedCache:
     def reserve(self, total_q: int, max_q_len: int, max_cache_len: int, shared_len: int = 0) -> None:
         """A workspace for attention calls of up to these sizes, with a prefix of up to shared_len rows.  Calls that overlap in
         time (two streams, two captured graphs) need a PagedCache, and with it a workspace, each; a captured graph needs the
-        workspace it was captured with, which a larger reservation replaces."""
+        workspace it was captured with, which a larger reservation replaces: keep a reference to it as long as the graph.  A
+        stream that a call was given as a number has to live until the workspace has been replaced."""
         n = calidrop_paged_attend_workspace_bytes(self.p, total_q, max_q_len, max_cache_len)
         if shared_len:
             n = max(n, calidrop_paged_attend_shared_workspace_bytes(self.p, total_q, max_q_len, max_cache_len, shared_len))
-        if self.workspace is None or self.workspace.nbytes < n:
+        if self._workspace is None or self._workspace.nbytes < n:
             self.workspace = torch.empty(n, dtype=torch.uint8, device=self.device)
 
     @staticmethod
@@ -643,10 +666,12 @@ class PagedCache:
         max_q_len = self._most(max_q_len, q_offsets, total)
         if max_cache_len is None:
             max_cache_len = self.capacity
-        ws = self.workspace
+        ws = self._workspace
         at_ws, n_ws = (None, 0) if ws is None else (ws.data_ptr(), ws.nbytes)
         L = _lib or lib()
         st = self._on_device(stream)
+        if st not in self._workspace_streams and ws is not None:
+            self._hold(ws, st)
         k, v, table, lens = self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.page_table.data_ptr(), self.cache_lens.data_ptr()
         if shared is None:
             status = L.calidrop_paged_attend(self._p, at_q, at_offsets, total, max_q_len, k, v, table, lens, max_cache_len, at_out, at_lse,

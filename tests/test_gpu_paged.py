@@ -556,6 +556,35 @@ def test_calls_on_two_streams_with_a_workspace_each():
     b.check()
 
 
+@pytest.mark.parametrize("by_argument", [True, False])
+@pytest.mark.parametrize("prefix", [0, 300])
+def test_a_larger_reservation_leaves_a_running_call_its_workspace(prefix, by_argument):
+    s = Setup([3000, 200, 900], [2, 1, 4], 8, 2, 128, "bf16", 16, prefix=prefix, seed=40)
+    size, old = s.cache.workspace.nbytes, s.cache.workspace.data_ptr()
+    x = torch.randn((4096, 4096), device=DEV)
+    more = (4 * s.total, 400, 3000) + ((prefix,) if prefix else ())
+    need = (cd.calidrop_paged_attend_shared_workspace_bytes if prefix else cd.calidrop_paged_attend_workspace_bytes)(s.cache.p, *more)
+    assert need > size
+    cached = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in (need,) + 4 * (size,)]     # so that nothing below waits for memory
+    del cached
+    torch.cuda.synchronize()
+    side, ended = torch.cuda.Stream(), torch.cuda.Event()
+    with torch.cuda.stream(side):
+        for _ in range(100):
+            x = x @ x / 64                                   # the call behind these starts when everything below is done
+        if not by_argument:
+            s.run()
+    if by_argument:
+        s.run(stream=side)
+    ended.record(side)
+    s.cache.reserve(*more)
+    taken = [torch.full((size,), 255, dtype=torch.uint8, device=DEV) for _ in range(4)]
+    early = not ended.query()
+    assert all(t.data_ptr() + size <= old or old + size <= t.data_ptr() for t in taken)
+    s.check()
+    assert early                                             # the call was still ahead when its memory could have been taken
+
+
 def test_a_workspace_of_the_largest_call_serves_the_others():
     s = Setup([2000, 100], [3, 1], 8, 2, 64, "bf16", 16, seed=35)
     s.cache.workspace = None

@@ -242,13 +242,13 @@ def test_calls_on_a_cache_off_the_current_gpu_are_refused():
 
 
 class Recorder:
-    """In the library's place: keeps the arguments of each call by name."""
+    """In the library's place: keeps the arguments of each call by name; sizes are the library's."""
 
     def __init__(self):
-        self.calls = []
+        self.calls, self.library = [], cd.lib()
 
     def __getattr__(self, name):
-        return lambda *args: self.calls.append((name, args)) or cd.OK
+        return getattr(self.library, name) if name.endswith("_bytes") else lambda *args: self.calls.append((name, args)) or cd.OK
 
 
 def recorded_cache(monkeypatch, **kw):
@@ -273,3 +273,37 @@ def test_without_a_bound_the_tokens_of_a_sequence_are_at_most_all():
             c.attend(q, q.clone(), lse, q_offsets=offsets, max_q_len=5)
         # max_new is argument 9 of append, max_q_len argument 4 of both others
         assert [args[9 if name.endswith("append") else 4] for name, args in lib.calls] == [want, want, want, 5, 5]
+
+
+def test_a_workspace_is_held_for_every_stream_that_uses_it(monkeypatch):
+    # the allocator hands freed memory out again on the stream it came from, unless it knows of the others
+    c, _ = recorded_cache(monkeypatch)
+    q, lse, prefix = torch.zeros((2, 4, 64), dtype=torch.bfloat16), torch.zeros((2, 4)), torch.zeros(2, dtype=torch.int32)
+    known = []
+    monkeypatch.setattr(cd, "_stream_object", lambda raw, device: raw)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, raw: known.append((t.data_ptr(), raw)))
+    c.reserve(2, 1, 32, 20)
+    first = c.workspace.data_ptr()
+    for stream in (None, 64, 64, None, 64):
+        c.attend(q, q.clone(), lse, stream=stream)
+    c.attend_shared(q, q.clone(), lse, prefix, 20, stream=128)
+    assert known == [(first, None), (first, 64), (first, 128)]            # once each: asking costs as much as a call's checks
+    small = c.workspace
+    c.reserve(500, 400, 32)
+    assert c.workspace is not small and c.workspace.nbytes > small.nbytes
+    c.attend(q, q.clone(), lse, stream=64)
+    other = torch.empty(1 << 20, dtype=torch.uint8)
+    c.workspace = other
+    c.attend(q, q.clone(), lse, stream=64)
+    assert known[3][1] == 64 and known[3][0] not in (first, other.data_ptr()) and known[4:] == [(other.data_ptr(), 64)]
+
+
+def test_workspaces_have_to_be_memory_of_the_cache_s_device():
+    c = cpu_cache()
+    c.workspace = torch.empty(512, dtype=torch.uint8)
+    for bad in (torch.empty(512, dtype=torch.uint8)[::2], torch.empty(512, dtype=torch.uint8, device="meta")):
+        with pytest.raises(ValueError, match="workspace"):
+            c.workspace = bad
+    assert c.workspace.nbytes == 512
+    c.workspace = None
+    assert c.workspace is None
