@@ -571,6 +571,7 @@ class PagedCache:
         self._fits(cache_lens, "cache_lens", torch.int32, (p.batch,))
         self.k_pages, self.v_pages, self.page_table, self.cache_lens = k_pages, v_pages, page_table, cache_lens
         self.workspace = None
+        self._grown = None                                    # told of the rows that cache_lens may have grown by
 
     @property
     def workspace(self):
@@ -655,6 +656,8 @@ class PagedCache:
             self._p, at_q, qs, k.data_ptr(), ks, v.data_ptr(), vs, at_offsets, total, max_new, at_positions, at_table, n_positions,
             self.k_pages.data_ptr(), self.v_pages.data_ptr(), self.page_table.data_ptr(), at_lens, at_new, at_out,
             self._on_device(stream)))
+        if self._grown is not None and at_new == at_lens:
+            self._grown(max_new if new_offsets is not None else 1)
 
     def _attend(self, shared, q, out, lse, q_offsets, max_q_len, max_cache_len, stream) -> None:
         fits = self._fits
@@ -740,8 +743,8 @@ class CompressBuffers:
         self.flags = torch.zeros((nb, Hq), dtype=torch.uint8, device=device)
 
     def _compressed(self):
-        # live rows of the longest cache as far as the host knows: what compress leaves, plus one per append.  decode says so in
-        # the budget of its call, hence no fewer than a budget may be.
+        # live rows of the longest cache as far as the host knows: what compress leaves, plus one per append, plus what is
+        # appended to paged() at most.  decode says so in the budget of its call, hence no fewer than a budget may be.
         self.live_rows = min(self.p.budget, self.max_seq_len)
         self._told_rows = max(self.live_rows, self.p.window + 1)
 
@@ -809,10 +812,13 @@ class CompressBuffers:
         calidrop_decode(p, q_t, self.k_c, self.v_c, offs, self.cache_lens, mcl, self.c_q, self.c_out,
                         self.c_lse, self.out, self.a_lse, self.flags, self.ws_decode, stream)
 
+    def _grow(self, rows: int):
+        self.live_rows = min(self.live_rows + rows, self.cap)
+        self._told_rows = max(min(self.live_rows, 1 << 24), self.p.window + 1)
+
     def append(self, k_new, v_new, stream=None):
         """Append the K/V rows of the token just generated ([batch][Hkv][D]) to every sequence."""
-        self.live_rows = min(self.live_rows + 1, self.cap)
-        self._told_rows = max(min(self.live_rows, 1 << 24), self.p.window + 1)
+        self._grow(1)
         calidrop_append(self.p, k_new, v_new, self.k_c, self.v_c, self.cache_offsets, self.cache_lens, stream)
 
     def recalibrate(self, q_t, k, v, seq_offsets, stream=None):
@@ -834,7 +840,9 @@ class CompressBuffers:
         pp = make_paged_params(dtype=p.dtype, batch=nb, n_q_heads=p.n_q_heads, n_kv_heads=p.n_kv_heads, head_dim=p.head_dim,
                                page_size=self.cap, n_pages=nb, max_pages=1, scale=p.scale, **kw)
         table = torch.arange(nb, dtype=torch.int32, device=self.out.device).view(nb, 1)
-        return PagedCache(pp, self.k_c.view(shape), self.v_c.view(shape), table, self.cache_lens)
+        pages = PagedCache(pp, self.k_c.view(shape), self.v_c.view(shape), table, self.cache_lens)
+        pages._grown = self._grow
+        return pages
 
     def region(self, region: int) -> torch.Tensor:
         off, nbytes = calidrop_compress_workspace_region(self.p, self.total_tokens,

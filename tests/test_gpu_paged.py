@@ -469,6 +469,33 @@ def test_prompt_then_compression_then_decode():
         assert (bufs.k_c.view(nb, hkv, cap, d)[:, :, budget + t] - want_k).abs().max() < 1e-5
 
 
+@pytest.mark.parametrize("at_once", [1, 200])
+def test_decode_after_rows_appended_as_pages_takes_the_form_of_their_number(at_once):
+    # 8 KV heads of 400 rows, then of 1000: one launch, then two, as after as many rows appended one by one
+    hkv, budget, n, appended = 8, 400, 450, 600
+    cp = cd.make_params(dtype="bf16", batch=1, n_q_heads=32, n_kv_heads=hkv, head_dim=128, window=16, budget=budget, pool_kernel=5)
+    g = torch.Generator(device=DEV).manual_seed(41)
+    win, k, v, q = (torch.randn(s, generator=g, device=DEV).bfloat16() for s in ((1, 32, 16, 128), (1, hkv, n, 128), (1, hkv, n, 128), (1, 32, 128)))
+    new = [torch.randn((appended, hkv, 128), generator=g, device=DEV).bfloat16() for _ in range(2)]
+    bufs, plain = (cd.CompressBuffers(cp, [n], DEV, extra_capacity=800) for _ in range(2))
+    for b in (bufs, plain):
+        b.compress(win, k, v, ints([0, n]))
+    form = lambda b: H.captured_launches(lambda: b.decode(q))
+    assert len(form(bufs)) == 1
+    pages = bufs.paged()
+    for t in range(0, appended, at_once):
+        k1, v1 = (x[t:t + at_once] for x in new)
+        pages.append(k1, v1, new_offsets=ints([0, at_once]), max_new=at_once)
+        for r in range(at_once):
+            plain.append(k1[r:r + 1], v1[r:r + 1])
+    assert form(bufs) == form(plain) and len(form(bufs)) == 2
+    for b in (bufs, plain):
+        b.decode(q)
+    torch.cuda.synchronize()
+    assert bufs.cache_lens.tolist() == [budget + appended] and torch.equal(bufs.k_c, plain.k_c) and torch.equal(bufs.v_c, plain.v_c)
+    assert torch.equal(bufs.out, plain.out) and torch.equal(bufs.a_lse, plain.a_lse)
+
+
 def decode_steps(steps, graph):
     """A loop of append + attend + attend_shared on the device, eager or replayed; the rows of every step."""
     nb, hq, hkv, d, page = 3, 8, 2, 128, 16

@@ -307,3 +307,41 @@ def test_workspaces_have_to_be_memory_of_the_cache_s_device():
     assert c.workspace.nbytes == 512
     c.workspace = None
     assert c.workspace is None
+
+
+def test_rows_appended_to_compressed_caches_as_pages_are_counted(monkeypatch):
+    # decode is told how many rows live, however they were appended
+    cp = cd.make_params(dtype="bf16", batch=2, n_q_heads=4, n_kv_heads=2, head_dim=64, window=8, budget=30, pool_kernel=5)
+    bufs, plain = (cd.CompressBuffers(cp, [100, 90], "cpu", extra_capacity=20) for _ in range(2))
+    lib = Recorder()
+    monkeypatch.setattr(cd, "_lib", lib)
+    monkeypatch.setattr(cd.PagedCache, "_on_device", lambda self, stream: stream)
+    pages = [bufs.paged(), bufs.paged(rot_dim=64)]
+    one, some = (torch.zeros((n, 2, 64), dtype=torch.bfloat16) for n in (2, 7))
+    q, table, offsets = torch.zeros((2, 4, 64), dtype=torch.bfloat16), torch.zeros((9, 64)), torch.tensor([0, 4, 7], dtype=torch.int32)
+
+    def told(b):
+        b.decode(q, stream=64)
+        return lib.calls[-1][1][0]._obj.budget
+
+    def grow(n, call):
+        call()
+        for _ in range(n):
+            plain.append(one, one, stream=64)
+        assert bufs.live_rows == plain.live_rows and told(bufs) == told(plain)
+
+    assert told(bufs) == 30
+    grow(1, lambda: pages[0].append(one, one))
+    grow(4, lambda: pages[1].append(some, some, new_offsets=offsets, max_new=4, rot_table=table))
+    assert told(bufs) == 35
+    grow(0, lambda: pages[0].append(one, one, new_lens=torch.zeros(2, dtype=torch.int32)))          # the lengths stay
+    grow(1, lambda: pages[0].append(one, one, new_lens=bufs.cache_lens))
+    grow(7, lambda: pages[0].append(some, some, new_offsets=offsets))
+    grow(7, lambda: pages[0].append(some, some, new_offsets=offsets))
+    assert told(bufs) == 50                                           # full
+    lib.calidrop_paged_append = lambda *args: cd.EINVAL
+    lib.calidrop_last_error = lambda: b"refused"
+    bufs._compressed(), plain._compressed()
+    with pytest.raises(cd.CalidropError):
+        pages[0].append(one, one)
+    grow(0, lambda: None)
