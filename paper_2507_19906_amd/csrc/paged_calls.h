@@ -176,7 +176,7 @@ int check_attend_sizes(const calidrop_paged_params* p, int64_t total_q, int32_t 
     return fail(CALIDROP_EUNSUPPORTED, "total_q * n_q_heads exceeds 2^29");
   const int64_t G = p->n_q_heads / p->n_kv_heads;
   if (max_q_len > (1 << 26) / G) return fail(CALIDROP_EUNSUPPORTED, "max_q_len * (n_q_heads / n_kv_heads) exceeds 2^26");
-  if ((max_q_len * G + 63) / 64 * p->n_kv_heads * p->batch > 1 << 23)           // with a prefix's, below 2^24 workgroups of 256 threads
+  if ((max_q_len * G + 63) / 64 * p->n_kv_heads * p->batch > 1 << 23)           // workgroups of 256 threads
     return fail(CALIDROP_EUNSUPPORTED, "batch * max_q_len * n_q_heads exceeds 2^29");
   if (max_cache_len > paged_capacity(p))
     return fail(CALIDROP_ESHAPE, "max_cache_len %d exceeds the max_pages * page_size = %lld rows of a table", max_cache_len,
@@ -184,10 +184,20 @@ int check_attend_sizes(const calidrop_paged_params* p, int64_t total_q, int32_t 
   if (max_cache_len > (1 << 30)) return fail(CALIDROP_EUNSUPPORTED, "max_cache_len %d exceeds 2^30", max_cache_len);
   return CALIDROP_OK;
 }
-int check_shared_sizes(const calidrop_paged_params* p, int32_t shared_len) {
+// No sequence has more tokens than the call, whatever the host's bound says.
+int64_t most_tokens(int64_t total_q, int64_t max_q_len) { return std::min(max_q_len, std::max<int64_t>(total_q, 1)); }
+
+// After check_attend_sizes.  A prefix adds as many blocks again to the first launch, and its second has four rows to a workgroup;
+// a launch holds fewer than 2^32 threads in a direction, 2^24 workgroups of 256.
+int check_shared_sizes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len, int32_t shared_len) {
   if (shared_len < 1) return fail(CALIDROP_ESHAPE, "shared_len must be >= 1 (got %d)", shared_len);
   if (shared_len > (1 << 30)) return fail(CALIDROP_EUNSUPPORTED, "shared_len %d exceeds 2^30", shared_len);
   if (p->window || p->sinks) return fail(CALIDROP_EUNSUPPORTED, "a shared prefix goes without window and sinks (got %d, %d)", p->window, p->sinks);
+  const int64_t q_len = most_tokens(total_q, max_q_len), rows = q_len * (p->n_q_heads / p->n_kv_heads);
+  if (paged_blocks(p, total_q, q_len, 0, shared_len).items * p->n_kv_heads >= 1 << 24)
+    return fail(CALIDROP_EUNSUPPORTED, "the prefix and the sequences together reach 2^24 blocks of queries");
+  if ((rows + 3) / 4 >= 1 << 24)
+    return fail(CALIDROP_EUNSUPPORTED, "with a prefix, max_q_len * (n_q_heads / n_kv_heads) exceeds 2^26 - 4");
   return CALIDROP_OK;
 }
 
@@ -242,7 +252,7 @@ int attend_entry(const calidrop_paged_params* p, const void* q, const int32_t* q
   a.pages = pages_of(p, page_table, p->max_pages);
   a.shared_table = shared_table; a.shared_len = shared_len;
   a.total_q = total_q; a.batch = p->batch; a.Hq = p->n_q_heads; a.G = p->n_q_heads / p->n_kv_heads;
-  a.max_q_len = q_offsets ? max_q_len : 1;
+  a.max_q_len = q_offsets ? static_cast<int>(most_tokens(total_q, max_q_len)) : 1;
   a.window = std::min(p->window, 1 << 30); a.sinks = std::min(p->sinks, 1 << 30);      // caches have no more rows
   a.sl2 = (p->scale > 0.f ? p->scale : 1.0f / std::sqrt(static_cast<float>(p->head_dim))) * cd::kLog2e;
   a.out = out; a.lse = lse;
@@ -353,7 +363,7 @@ int calidrop_paged_attend(const calidrop_paged_params* p, const void* q, const i
 size_t calidrop_paged_attend_shared_workspace_bytes(const calidrop_paged_params* p, int64_t total_q, int32_t max_q_len,
                                                     int32_t max_cache_len, int32_t shared_len) {
   if (check_paged(p) != CALIDROP_OK || check_attend_sizes(p, total_q, max_q_len, max_cache_len) != CALIDROP_OK ||
-      check_shared_sizes(p, shared_len) != CALIDROP_OK) return 0;
+      check_shared_sizes(p, total_q, max_q_len, shared_len) != CALIDROP_OK) return 0;
   return attend_bytes(p, total_q, max_q_len, max_cache_len, shared_len);
 }
 
@@ -364,7 +374,7 @@ int calidrop_paged_attend_shared(const calidrop_paged_params* p, const void* q, 
   int rc;
   if ((rc = check_paged(p))) return rc;
   if ((rc = check_attend_sizes(p, total_q, max_q_len, max_cache_len))) return rc;
-  if ((rc = check_shared_sizes(p, shared_len))) return rc;
+  if ((rc = check_shared_sizes(p, total_q, max_q_len, shared_len))) return rc;
   if (!shared_table) return fail(CALIDROP_EINVAL, "shared_table is NULL");
   return attend_entry(p, q, q_offsets, total_q, max_q_len, k_pages, v_pages, shared_table, shared_len, page_table, cache_lens,
                       max_cache_len, out, lse, workspace, workspace_bytes, attend_bytes(p, total_q, max_q_len, max_cache_len, shared_len),

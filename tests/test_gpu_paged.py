@@ -301,6 +301,16 @@ def test_offsets_without_a_bound(dtype, lens, nq, prefix):
     s.run().check()
 
 
+@pytest.mark.parametrize("lens,nq,prefix", [([70, 33, 9], [1, 3, 2], 0), ([4000, 300], [30, 2], 0), ([30, 70, 12], [20, 1, 12], 333), ([5, 9], [1, 1], 4000)])
+def test_a_bound_far_above_the_tokens(lens, nq, prefix):
+    # the largest bound there is (2^26 rows of a KV head): launches are sized by the tokens of the call
+    s = Setup(lens, nq, 8, 2, 128, "bf16", 16, prefix=prefix, seed=42)
+    s.most["max_q_len"] = 1 << 24
+    s.cache.reserve(s.total, s.most["max_q_len"], max(lens), prefix)
+    assert all(x * y * z <= 2048 for x, y, z, _ in H.captured_launches(lambda: s.run()))
+    s.run().check()
+
+
 # ---- append -------------------------------------------------------------------------------------------------------------------
 
 def append_case(dtype, d, hq, hkv, page, lens, nq, rot, pairs, seed, max_pages=None, one=False, positions=True, with_q=True, in_place=False, bad=False):

@@ -345,3 +345,40 @@ def test_rows_appended_to_compressed_caches_as_pages_are_counted(monkeypatch):
     with pytest.raises(cd.CalidropError):
         pages[0].append(one, one)
     grow(0, lambda: None)
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 1), (16, 1), (32, 8)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_calls_behind_a_prefix_launch_fewer_than_2_to_32_threads(dtype, hq, hkv):
+    # the joining launch has four rows to a workgroup of 256 threads: 2^26 - 4 rows of a KV head at most
+    p = params(dtype=dtype, batch=1, n_q_heads=hq, n_kv_heads=hkv, head_dim=64)
+    G = hq // hkv
+    for tokens in (1 << 26, (1 << 26) - 1, (1 << 26) - 3, (1 << 26) - 4, (1 << 26) - 16):
+        tokens //= G
+        for total in {tokens, min(tokens, (1 << 29) // hq)}:
+            joined = min(tokens, total) * G                            # no sequence has more tokens than the call
+            rows = 128 if dtype == "bf16" else 64                       # of a block
+            blocks = (-(-joined // rows) - (-total * G // rows)) * hkv
+            args = shared_args(total_q=total, max_q_len=tokens, workspace_bytes=256)
+            size = lambda: cd.calidrop_paged_attend_shared_workspace_bytes(p, total, tokens, 300, 50)
+            if total * hq > 1 << 29 or (tokens * G + 63) // 64 * hkv > 1 << 23 or -(-joined // 4) >= 1 << 24 or blocks >= 1 << 24:
+                assert cd.lib().calidrop_paged_attend_shared(ctypes.byref(p), *args) == cd.EUNSUPPORTED, (tokens, total)
+                with pytest.raises(cd.CalidropError, match="2\\^"):
+                    size()
+            else:
+                assert cd.lib().calidrop_paged_attend_shared(ctypes.byref(p), *args) == cd.EWORKSPACE, (tokens, total)
+                assert size() > 256
+
+
+def test_blocks_of_a_prefix_and_of_the_sequences_launch_fewer_than_2_to_32_threads():
+    # 2^23 workgroups of each: fp32 blocks of 64 rows behind a prefix as many again; bf16 blocks of 128 are half as many
+    for dtype, code in (("fp32", cd.EUNSUPPORTED), ("bf16", cd.EWORKSPACE)):
+        p = params(dtype=dtype, batch=1 << 11, n_q_heads=32, n_kv_heads=32, head_dim=64, n_pages=1, max_pages=20)
+        args = dict(total_q=1 << 24, max_q_len=1 << 13, workspace_bytes=256)
+        assert cd.lib().calidrop_paged_attend_shared(ctypes.byref(p), *shared_args(**args)) == code
+        assert cd.lib().calidrop_paged_attend(ctypes.byref(p), *attend_args(**args)) == cd.EWORKSPACE
+
+
+def test_a_loose_bound_of_the_tokens_needs_a_workspace_but_no_larger_launch():
+    p = params(batch=3)
+    assert cd.lib().calidrop_paged_attend_shared(ctypes.byref(p), *shared_args(total_q=7, max_q_len=1 << 21, workspace_bytes=256)) == cd.EWORKSPACE
