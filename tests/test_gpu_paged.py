@@ -479,6 +479,29 @@ def test_prompt_then_compression_then_decode():
         assert (bufs.k_c.view(nb, hkv, cap, d)[:, :, budget + t] - want_k).abs().max() < 1e-5
 
 
+@pytest.mark.parametrize("prefix", [0, 90])
+def test_functions_of_the_module_and_the_cache_agree(prefix):
+    s, t = (Setup([70, 33, 9], [3, 1, 2], 8, 2, 64, "bf16", 16, prefix=prefix, seed=43) for _ in range(2))
+    new = [torch.randn((3, 2, 64), generator=torch.Generator().manual_seed(44)).bfloat16().to(DEV) for _ in range(2)]
+    a, b = s.cache, t.cache
+    a.append(*new)
+    cd.calidrop_paged_append(b.p, None, 0, new[0], 128, new[1], 128, None, 3, 1, None, None, 0, b.k_pages, b.v_pages, b.page_table, b.cache_lens,
+                             b.cache_lens, None)
+    a.cache_lens -= 1                                       # the same queries at their own rows again
+    b.cache_lens -= 1
+    s.run()
+    head, tail = (t.qd, t.q_off, t.total, 3, b.k_pages, b.v_pages), (b.page_table, b.cache_lens, 70, t.out, t.lse, b.workspace)
+    if prefix:
+        cd.calidrop_paged_attend_shared(b.p, *head, t.shared_table, prefix, *tail)
+    else:
+        cd.calidrop_paged_attend(b.p, *head, *tail)
+    s.check()
+    t.check()
+    assert torch.equal(s.out, t.out) and torch.equal(s.lse, t.lse) and a.cache_lens.tolist() == b.cache_lens.tolist() == [70, 33, 9]
+    for x, y in ((a.k_pages, b.k_pages), (a.v_pages, b.v_pages)):
+        assert torch.equal(x.nan_to_num(0.25), y.nan_to_num(0.25))
+
+
 @pytest.mark.parametrize("at_once", [1, 200])
 def test_decode_after_rows_appended_as_pages_takes_the_form_of_their_number(at_once):
     # 8 KV heads of 400 rows, then of 1000: one launch, then two, as after as many rows appended one by one

@@ -382,3 +382,26 @@ def test_blocks_of_a_prefix_and_of_the_sequences_launch_fewer_than_2_to_32_threa
 def test_a_loose_bound_of_the_tokens_needs_a_workspace_but_no_larger_launch():
     p = params(batch=3)
     assert cd.lib().calidrop_paged_attend_shared(ctypes.byref(p), *shared_args(total_q=7, max_q_len=1 << 21, workspace_bytes=256)) == cd.EWORKSPACE
+
+
+def test_functions_and_cache_hand_the_library_the_same(monkeypatch):
+    c, lib = recorded_cache(monkeypatch)
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)
+    q, k, v = (torch.zeros((7, h, 64), dtype=torch.bfloat16) for h in (4, 2, 2))
+    part = torch.zeros((7, 5, 64), dtype=torch.bfloat16)[:, 1:3]           # of a projection: tokens 320 elements apart
+    lse, table, offs, pos, prefix, lens, out = torch.zeros((7, 4)), torch.zeros((9, 32)), i32(3), i32(7), i32(2), i32(2), q.clone()
+    c.workspace = torch.empty(1 << 22, dtype=torch.uint8)
+    monkeypatch.setattr(c, "_hold", lambda ws, st: None)
+    c.append(part, v, q=q, q_out=out, new_offsets=offs, max_new=5, positions=pos, rot_table=table, new_lens=lens, stream=64)
+    cd.calidrop_paged_append(c.p, q, 256, part, 320, v, 128, offs, 7, 5, pos, table, 9, c.k_pages, c.v_pages, c.page_table, c.cache_lens, lens, out, 64)
+    c.append(k, v, new_offsets=offs, max_new=5, stream=64)
+    cd.calidrop_paged_append(c.p, None, 0, k, 128, v, 128, offs, 7, 5, None, None, 0, c.k_pages, c.v_pages, c.page_table, c.cache_lens, c.cache_lens, None, 64)
+    c.attend(q, out, lse, q_offsets=offs, max_q_len=6, max_cache_len=30, stream=64)
+    cd.calidrop_paged_attend(c.p, q, offs, 7, 6, c.k_pages, c.v_pages, c.page_table, c.cache_lens, 30, out, lse, c.workspace, 64)
+    c.attend_shared(q, out, lse, prefix, 20, q_offsets=offs, max_q_len=6, stream=64)
+    cd.calidrop_paged_attend_shared(c.p, q, offs, 7, 6, c.k_pages, c.v_pages, prefix, 20, c.page_table, c.cache_lens, 32, out, lse, c.workspace, 64)
+    value = lambda x: getattr(x, "value", x)                            # a pointer, however it was wrapped
+    for (name, a), (name2, b) in zip(lib.calls[::2], lib.calls[1::2]):
+        assert name == name2 and ctypes.addressof(a[0]._obj) == ctypes.addressof(b[0]._obj)
+        assert [value(x) for x in a[1:]] == [value(x) for x in b[1:]]
+    assert len(lib.calls) == 8
