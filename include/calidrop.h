@@ -35,6 +35,9 @@
  *     budget <= 2^24 (CALIDROP_EUNSUPPORTED otherwise).
  *   - Accumulation is always fp32; `dtype` is the storage type of Q/K/V, the compressed cache
  *     and the decode output.  The calibration state is always fp32.
+ *   - In bf16, attention rounds each softmax weight to bf16 (by at most 2^-8 of it) for the product with V, the type
+ *     the matrix cores take; the weights' sum and the log-sum-exp are of the unrounded ones.  An output is off by at
+ *     most 2^-8 of the weighted mean of |V| so, ahead of its own rounding.  fp32 rounds no weight.
  *   - Logits are scaled by 1/sqrt(head_dim) (Eq. 2) unless `scale` is non-zero.
  */
 #ifndef CALIDROP_H
