@@ -526,9 +526,9 @@ struct PagedWave {
 // Few queries, up to 16 (token, head) rows: the 4 waves of a workgroup take its 32-row tiles in turn, K and V from memory to
 // registers without LDS, the page of the next tile's rows looked up by one lane each meanwhile.
 // Bound by the bytes of K and V: 64 sequences of 16001 rows, D = 128 in bf16, 32 query and 8 KV heads, 667 us, 6.3 TB/s; of 1000
-// to 16000 rows 348 us, 6.1 TB/s; one of 32768 rows 25 us and 5 for the launch that joins the parts, 4.1 TB/s together.  Tried
-// and no faster: K and V of a tile requested while the one before is worked on (31.3 for 32.2 us, fp32 121 for 107), 512, 640
-// or 1024 places for shares instead of 768 (bf16: three workgroups on a compute unit).
+// to 16000 rows 348 us, 6.1 TB/s; one of 32768 rows 25 us, 5.4 TB/s, and 5 for the launch that joins the parts.  In fp32 one of
+// 16000 rows 42 us, 3.1 TB/s; 32 of 1000 to 8000 rows 220 us, 5.5 TB/s.  Tried and no faster: K and V of a tile requested while
+// the one before is worked on (31.3 for 32.2 us, fp32 121 for 107).
 constexpr int kStreamRows = 16, kStreamTile = 32;
 
 template <typename T, int D, bool kShare>
@@ -577,7 +577,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) void paged_stream_kern
 #pragma unroll
         for (int t2 = 0; t2 < 2; ++t2) mma_step<T>(sc[t2], kf[t2][kk], w.qf[kk]);
       w.template weigh<2>(sc, 0, base, from, to, pos, a, c);
-      // The weights are rounded to the type of V, the precision the matrix cores take them in.
+      // The weights are rounded to the type of V, the precision the matrix cores take them in: each by 2^-8 of it at most in bf16,
+      // to either side, so that a mean over many rows loses less.  Their sum is taken ahead of the rounding: the log-sum-exp, which
+      // other calls join results and score rows by, is as exact as in fp32.
       if constexpr (W::kBf16) {
         const u32x4 pf = {pack_bf16x2(sc[0][0], sc[0][1]), pack_bf16x2(sc[0][2], sc[0][3]), pack_bf16x2(sc[1][0], sc[1][1]), pack_bf16x2(sc[1][2], sc[1][3])};
 #pragma unroll
@@ -667,7 +669,8 @@ struct PagedTiles {
   // 2 (V % 4)).
   static __device__ __forceinline__ int swizzle_k(int r) { return kRowBytes == 128 ? (r >> 1) & 7 : r & 15; }
   static __device__ __forceinline__ int swizzle_v(int r) { return !kBf16 ? 0 : D == 128 ? 4 * (r & 3) : 2 * (r & 2); }
-  // the wave's rows of K or V of a tile on their way to `dst`; swizzle(row % 8): XORed to the index of a 16-byte piece
+  // the wave's rows of K or V of a tile on their way to `dst`; swizzle(r), r the row among the wave's: XORed to the index of a
+  // 16-byte piece
   template <typename S>
   __device__ __forceinline__ void issue(const void* src, uint32_t rid, char* dst, S&& swizzle) const {
     const int sub = lane / kChunks, piece = lane % kChunks;
@@ -710,6 +713,8 @@ __device__ __forceinline__ f32x16 mma32(const u32x4& a, const u32x4& b, const f3
 // Bound by the chip's power: a prompt of 16384 tokens, D = 128, 32 query and 8 KV heads, runs at 2160 us, 1020 TFLOP/s, with the
 // matrix cores busy half of the time at 1.75 GHz (a library's product of 8192 x 8192 matrices: 1314 TFLOP/s, 70 % at 1.67 GHz).
 // What raises the share of the time lowers the clock: without the logits ahead 45 % at 1.86 GHz, 2230 us.  Tried and no faster:
+// (The shared forms keep 16 to 26 scalar registers in lanes of vector ones; no vector register is spilled.)  Short prompts are bound by the chain of tiles of their last block, 1.35 us each where it has a compute unit to itself:
+// 2048 tokens 56 us, 611 TFLOP/s, of 32 tiles; 4096 tokens 148 us, 930 TFLOP/s.  Tried and no faster for 16384 tokens:
 // schedules given to the compiler, 8 waves of 32 rows to a workgroup, 4 waves of 64 (half the reads of LDS, one wave on a SIMD
 // and 36 % at 2.1 GHz: 2470 us; with D = 64 up to 10 % faster on prompts beyond 8000 tokens, 20 to 60 % slower on short ones).
 template <int D, bool kShare>
@@ -823,7 +828,7 @@ __global__ __launch_bounds__(256, D == 64 && !kShare ? 3 : 2) void paged_tile_ke
         for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) { sc[kb][e] = fast_exp2(sc[kb][e] * a.sl2 - shift); l += sc[kb][e]; }
-          // rounded to bf16, what the matrix cores take
+          // rounded to bf16, what the matrix cores take, after their sum, as in the streaming kernel
 #pragma unroll
           for (int sh = 0; sh < 2; ++sh)
 #pragma unroll
@@ -891,7 +896,10 @@ __global__ __launch_bounds__(256, D == 64 && !kShare ? 3 : 2) void paged_tile_ke
 }
 
 // The same in fp32, tiles of 32 rows, products of 16 x 16 x 4: the layouts of the streaming kernel, with 16 rows to a wave and the
-// operands read from LDS 16 rows of the cache at a time.  Bound by the products.
+// operands read from LDS 16 rows of the cache at a time.  Logits, maximum, rescaling, weights and the product with V of 16 rows
+// follow one another, and nothing but the other wave of a SIMD works meanwhile: D = 128, 32 query and 8 KV heads, a prompt of 4096
+// tokens 1313 us, 105 TFLOP/s (a large fp32 matrix product: 153), 512 queries at 8192 rows 643 us, 104; a prompt of 1024 114 us, 75: a
+// block's chain of tiles, 3 us each, shared out and joined.
 template <int D, bool kShare>
 __global__ __launch_bounds__(256, 2) void paged_tile32_kernel(PagedAttendArgs a) {
   using P = PagedTiles<float, D>;

@@ -69,7 +69,12 @@ cd::Pages pages_of(const calidrop_paged_params* p, const int32_t* table, int64_t
 // How an attention launch is cut up.  Up to 16 (token, head) rows stream the cache from memory to registers, more share tiles of
 // it in LDS.
 struct PagedPlan { bool stream; int rows, tile, least_shift; int64_t blocks, prefix, items, share, most_tiles; };      // share 0: a workgroup per block
-constexpr int kPagedStreamPlaces = 768, kPagedTilePlaces = 512;        // workgroups the chip holds at a time (bf16, D = 128)
+// Workgroups that share the tiles of all KV heads: what the chip holds at a time of the bf16 kernels for D = 128.  Others fit in other
+// numbers: of streams in fp32 with D = 128 512, in bf16 with D = 64 1024; of tiles in fp32 with D = 64 1280.  Streams measured with 512,
+// 768 and 1024 (8 KV heads, us): fp32, D = 128, one sequence of 16000 rows 32.6, 41.7, 35.4, 4 of 8000 56.4, 65.0, 58.9, 32 of 1000 to
+// 16000 404, 404, 395; bf16, D = 64, 4 of 16000 31.7, 31.0, 29.8, 16 of 8000 54.3, 51.4, 51.5; fp32, D = 64, 16 of 4000 55.1, 54.0,
+// 59.2; bf16, D = 128: 512, 640 and 1024 no faster.  768 is within 8 % of the best but in fp32 with D = 128, where it costs up to 28 %.
+constexpr int kPagedStreamPlaces = 768, kPagedTilePlaces = 512;
 constexpr int64_t kPagedMostItems = 4096;                              // every workgroup adds up their tiles
 
 // Most tiles that a block can need (cd::KeyTiles): under a window, the rows of the window and of the sinks can begin and end
@@ -103,8 +108,9 @@ PagedPlan paged_blocks(const calidrop_paged_params* p, int64_t total_q, int64_t 
 }
 
 // A workgroup per block, or the tiles of a KV head shared evenly (and a launch that joins the parts): whichever is expected to take
-// less time, from the longest cache the host knows of.  Measured in 188 calls (1 to 64 sequences, 1 to 4096 queries, caches of 100
-// to 16512 rows, both types and head dimensions, 32 query and 8 KV heads), us a call, own block / shared:
+// less time, from the longest cache the host knows of.  Measured in 191 calls (1 to 64 sequences, 1 to 4096 queries, caches of 100
+// to 16512 rows, both types and head dimensions, 32 query and 8 KV heads), where the choice is 0.8 % behind the better form on average
+// (21 % at most, one fp32 query of 300 rows); us a call, own block / shared:
 //   streams of one query, bf16, D = 128: 1 sequence of 300 rows 9.1 / 11.9, of 600 13.3 / 11.9, of 4000 78 / 14; 16 of 600 17.7 /
 //   20.1, of 1000 26.7 / 21.7, of 16000 364 / 174; 64 of 1000 46.6 / 55.3, of 4000 172 / 178.
 //   tiles, bf16, D = 128: 64 queries at 1000 rows 29 / 24, at 16000 359 / 44; 512 queries of a prompt 17.6 / 32.5, at 8512 rows
