@@ -712,15 +712,14 @@ __device__ __forceinline__ f32x16 mma32(const u32x4& a, const u32x4& b, const f3
 //
 // Bound by the chip's power: a prompt of 16384 tokens, D = 128, 32 query and 8 KV heads, runs at 2160 us, 1020 TFLOP/s, with the
 // matrix cores busy half of the time at 1.75 GHz (a library's product of 8192 x 8192 matrices: 1314 TFLOP/s, 70 % at 1.67 GHz).
-// What raises the share of the time lowers the clock: without the logits ahead 45 % at 1.86 GHz, 2230 us.  Tried and no faster:
+// What raises the share of the time lowers the clock: without the logits ahead 45 % at 1.86 GHz, 2230 us.
 // (The shared forms keep 16 to 26 scalar registers in lanes of vector ones; no vector register is spilled.)
 //
 // Short prompts are bound by the chain of tiles of their last block, 1.35 us each where it has a compute unit to itself: 2048 tokens,
 // 32 tiles, 56 us, 611 TFLOP/s; 4096 tokens 148 us, 930 TFLOP/s.
 //
-// Tried for 16384 tokens and no faster:
-// schedules given to the compiler, 8 waves of 32 rows to a workgroup, 4 waves of 64 (half the reads of LDS, one wave on a SIMD
-// and 36 % at 2.1 GHz: 2470 us; with D = 64 up to 10 % faster on prompts beyond 8000 tokens, 20 to 60 % slower on short ones).
+// Tried for 16384 tokens and no faster: schedules given to the compiler, 8 waves of 32 rows to a workgroup, 4 waves of 64 (half the
+// reads of LDS, one wave on a SIMD and 36 % at 2.1 GHz: 2470 us; with D = 64 up to 10 % faster on prompts beyond 8000 tokens, 20 to 60 % slower on short ones).
 template <int D, bool kShare>
 __global__ __launch_bounds__(256, D == 64 && !kShare ? 3 : 2) void paged_tile_kernel(PagedAttendArgs a) {
   using P = PagedTiles<bf16_t, D>;
